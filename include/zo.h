@@ -421,6 +421,122 @@ int32_t zo_qk_norm_rope(const zo_batch* batch, void* Q, int64_t ldq, void* K, in
                         const float* gamma_q, const float* gamma_k, float norm_eps,
                         float rope_theta, zo_dtype dtype, void* stream);
 
+/*
+ * ---- Decoding from a paged key/value cache --------------------------------------
+ * The other query shape of Sec. 2.2: a candidate continues a prompt token by token and the
+ * answer is what is rewarded.  A decode step runs the probe linears on one row per sequence
+ * (every sequence under its own candidate); what joins them here is the cache of earlier
+ * keys and values, attention over it, and the draw of the next token.  The paper inherits
+ * these from its serving engine and does not spell them out; the definitions are below.
+ *
+ * The cache of one layer.  A sequence's positions 0, 1, ... lie in pages of page_size
+ * positions anywhere in a pool; page_table names the page of every page_size positions.
+ *
+ *   K, V        [n_pages][n_kv_heads][page_size][head_dim] of type dtype, 16-byte aligned
+ *   page_table  [n_seqs][max_pages] page ids
+ *   kv_len      [n_seqs] positions of every sequence, the rows of the present call included:
+ *               row t of sequence i has position kv_len[i] - (cu[i+1] - t)
+ *   host_*      optional host copies, used to validate a call only; may be NULL
+ *
+ * page_size is a power of two from 16 to 1024, and max_pages * page_size at most 2^30.  A page
+ * may serve several sequences (a shared prefix), but a position that a call writes must be named
+ * by one of its rows only.  On the device nothing outside the pool is touched, whatever the tables
+ * hold: a position below 0, beyond max_pages * page_size or on a page outside [0, n_pages) is
+ * neither written nor seen.  Slots behind a sequence's last position are never used, so what they
+ * hold (NaN included) does not matter.
+ */
+typedef struct zo_cache {
+  int32_t n_pages;
+  int32_t page_size;
+  int32_t n_kv_heads, head_dim;
+  zo_dtype dtype;
+  int32_t max_pages;
+  void* K;
+  void* V;
+  const int32_t* page_table;
+  const int32_t* kv_len;
+  const int32_t* host_page_table;
+  const int32_t* host_kv_len;
+} zo_cache;
+
+/*
+ * Per-head norm, rotary embedding and storing of new rows: as zo_qk_norm_rope, but at the row's
+ * position in the cache (not its offset in the call), out of place, and the keys and values go to
+ * their slots of the pages:
+ *   q, k <- x / sqrt(mean(x^2) + norm_eps) * gamma        (both gammas NULL: no norm)
+ *   (x[i], x[i + head_dim/2]) <- rotation of that pair by pos * rope_theta^(-2i/head_dim)   (rope_theta <= 0: none)
+ *   Qout[t] = q;  K[page][g][slot] = k, V[page][g][slot] = v of kv head g
+ * Of `batch` only n_tokens, n_seqs and cu_seqlens are read.  Q, Qout: [n_tokens x n_heads*head_dim];
+ * K, V: [n_tokens x n_kv_heads*head_dim], of the cache's dtype; the three may be column ranges of one
+ * fused projection output.  Qout may be Q itself (same pointer and leading dimension); otherwise it
+ * overlaps none of the inputs.  head_dim even, <= 256; one rounding to dtype.  Angles are formed in
+ * double precision, so that far positions keep theirs.  No workspace.
+ * Refused with ZO_ERR_INDEX where the host copies show it: a kv_len smaller than the sequence's rows
+ * or beyond its pages, a page of a position in use outside the pool.
+ */
+int32_t zo_cache_append(const zo_batch* batch, const void* Q, int64_t ldq, const void* K, int64_t ldk,
+                        const void* V, int64_t ldv, int32_t n_heads, const float* gamma_q,
+                        const float* gamma_k, float norm_eps, float rope_theta, const zo_cache* cache,
+                        void* Qout, int64_t ldqo, void* stream);
+
+/*
+ * Attention of new rows over the cache (their own keys and values stored by zo_cache_append first):
+ *   O[t, h] = sum_j softmax_j(scale * <Q[t, h], K[j, g]>) V[j, g],   g = h / (n_heads / n_kv_heads),
+ *   j over the positions 0 .. pos(t) of the row's sequence
+ * A row that sees no position (kv_len 0, or only pages outside the pool) gets zeros.  Laid out for one
+ * row per sequence; several rows of a sequence each read its cache.
+ * ZO_BF16: head_dim 64, 128 or 256; products on bf16 MFMA with fp32 accumulation, softmax in fp32, weights
+ * rounded to bf16 before the second product.  ZO_F32: head_dim <= 256, fp32 throughout.
+ * A long row is cut into ranges that are joined afterwards; the ranges depend on the row's own
+ * position alone, so its bits depend neither on the batch nor on the size of the page table.
+ * The workspace holds the ranges' partial results: max_len is max_pages * page_size of the cache.
+ */
+size_t zo_attention_paged_workspace_bytes(int32_t n_tokens, int32_t n_heads, int32_t head_dim, int32_t max_len,
+                                          zo_dtype dtype);
+
+int32_t zo_attention_paged(const zo_batch* batch, const void* Q, int64_t ldq, int32_t n_heads, float scale,
+                           const zo_cache* cache, void* O, int64_t ldo, void* workspace, size_t workspace_bytes,
+                           void* stream);
+
+/*
+ * Draws one token per row of logits [n_rows x vocab] (row-major, ld elements) from given uniforms.
+ * With z the row's logits (NaN counts as -infinity), M their maximum and T its temperature,
+ *   w_i = exp((z_i - M) / T)                   (M infinite: 1 for the tokens at M, 0 for the others)
+ *   order: z descending, equal logits by ascending index; tokens at -infinity are left out
+ *   kept = the first max(1, min(k, n_p, n_m)) tokens of that order, with
+ *     k    top_k[t]                                                       (<= 0: no limit)
+ *     n_p  how many of the first k have less than top_p[t] * Z_k before them, Z_k = the w of the first k
+ *          (top_p >= 1 or NaN: no limit)
+ *     n_m  how many have w_i >= min_p[t]                                  (min_p <= 0 or NaN: no limit)
+ *   tokens[t] = the lowest kept index i with  sum of w_j over kept j <= i  >  u[t] * Z,  Z = the w of all kept
+ *               (the last kept token with a weight where rounding leaves none)
+ *   prob[t]   = w / Z of that token;  n_kept[t] = number of kept tokens
+ * temperature[t] <= 0 or NaN: the first token of the order (prob 1, n_kept 1).  A row without a token above
+ * -infinity: token -1, prob 0, n_kept 0.  u is clamped to [0, 1] (NaN: 0).
+ *   temperature, u  fp32 [n_rows];  top_k int32 [n_rows], top_p, min_p fp32 [n_rows], each may be NULL: no limit
+ *   tokens int32 [n_rows];  prob fp32 [n_rows] and n_kept int32 [n_rows], each may be NULL
+ * Weights and their sums are formed in 64 bits.  vocab up to 2^19.  The logits need no alignment beyond their type's.
+ */
+size_t zo_sample_workspace_bytes(int32_t n_rows, int32_t vocab, zo_dtype dtype);
+
+int32_t zo_sample(const void* logits, int64_t ld, int32_t n_rows, int32_t vocab, zo_dtype dtype,
+                  const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+                  const float* u, int32_t* tokens, float* prob, int32_t* n_kept, void* workspace,
+                  size_t workspace_bytes, void* stream);
+
+/*
+ * The rows that tokens start with: X[t] = E[tokens[t]] (+ E_pos[pos[t]] with a table of learned positions;
+ * the sum in fp32, rounded once) and pos_next[t] = pos[t] + 1.  A token outside [0, vocab) (the -1 of
+ * zo_sample) or a position outside [0, n_pos) contributes zeros.
+ *   tokens int32 [n_rows];  pos int32 [n_rows] (may be NULL when neither E_pos nor pos_next is given)
+ *   E [vocab x d] ld lde, E_pos [n_pos x d] ld ldp (NULL: none), X [n_rows x d] ld ldx, of type dtype
+ *   pos_next int32 [n_rows] (may be NULL; may be pos itself, e.g. the kv_len of a decode loop)
+ * No workspace.
+ */
+int32_t zo_embed_rows(const int32_t* tokens, const int32_t* pos, int32_t n_rows, const void* E, int64_t lde,
+                      int32_t vocab, const void* E_pos, int64_t ldp, int32_t n_pos, int32_t d, zo_dtype dtype,
+                      void* X, int64_t ldx, int32_t* pos_next, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

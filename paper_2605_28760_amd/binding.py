@@ -47,6 +47,13 @@ class zo_sched(C.Structure):
                 ("append", C.c_int32), ("reserved", C.c_int32)]
 
 
+class zo_cache(C.Structure):
+    _fields_ = [("n_pages", C.c_int32), ("page_size", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("dtype", C.c_int), ("max_pages", C.c_int32), ("K", C.c_void_p), ("V", C.c_void_p),
+                ("page_table", C.c_void_p), ("kv_len", C.c_void_p), ("host_page_table", C.c_void_p),
+                ("host_kv_len", C.c_void_p)]
+
+
 class ZoError(RuntimeError):
     def __init__(self, status, message):
         super().__init__("zo status %d: %s" % (status, message))
@@ -96,6 +103,18 @@ _PROTOS = {
     "zo_qk_norm_rope": (C.c_int32, [C.POINTER(zo_batch), C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int32,
                                     C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_float, C.c_float, C.c_int,
                                     C.c_void_p]),
+    "zo_cache_append": (C.c_int32, [C.POINTER(zo_batch), C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p,
+                                    C.c_int64, C.c_int32, C.c_void_p, C.c_void_p, C.c_float, C.c_float,
+                                    C.POINTER(zo_cache), C.c_void_p, C.c_int64, C.c_void_p]),
+    "zo_attention_paged_workspace_bytes": (C.c_size_t, [C.c_int32] * 4 + [C.c_int]),
+    "zo_attention_paged": (C.c_int32, [C.POINTER(zo_batch), C.c_void_p, C.c_int64, C.c_int32, C.c_float,
+                                       C.POINTER(zo_cache), C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "zo_sample_workspace_bytes": (C.c_size_t, [C.c_int32, C.c_int32, C.c_int]),
+    "zo_sample": (C.c_int32, [C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_int] + [C.c_void_p] * 9
+                  + [C.c_size_t, C.c_void_p]),
+    "zo_embed_rows": (C.c_int32, [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p,
+                                  C.c_int64, C.c_int32, C.c_int32, C.c_int, C.c_void_p, C.c_int64, C.c_void_p,
+                                  C.c_void_p]),
     "zo_bank_update_multi": (C.c_int32, [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
                                          C.c_float, C.c_void_p, C.c_void_p, C.c_int32, C.c_int, C.c_void_p]),
 }
@@ -272,6 +291,57 @@ def zo_qk_norm_rope(batch, Q, ldq, K, ldk, n_heads, n_kv_heads, head_dim, gamma_
                     dtype, stream=None):
     _check(lib().zo_qk_norm_rope(C.byref(batch), _ptr(Q), ldq, _ptr(K), ldk, n_heads, n_kv_heads, head_dim,
                                  _ptr(gamma_q), _ptr(gamma_k), norm_eps, rope_theta, dtype, _stream(stream)))
+
+
+def make_cache(K, V, dtype, page_table, kv_len, host_page_table=None, host_kv_len=None):
+    """Fills a zo_cache from pools K, V [n_pages, n_kv_heads, page_size, head_dim], page_table [n_seqs, max_pages] and
+    kv_len [n_seqs] on the device (and optional host numpy mirrors of the last two).  The caller keeps the tensors
+    alive for as long as the struct is used."""
+    c = zo_cache()
+    for what, t in (("K", K), ("V", V), ("page_table", page_table), ("kv_len", kv_len)):
+        if not t.is_contiguous():
+            raise ValueError("%s is not contiguous" % what)
+    if tuple(K.shape) != tuple(V.shape) or K.dtype != V.dtype:
+        raise ValueError("K and V differ in shape or type")
+    if page_table.element_size() != 4 or kv_len.element_size() != 4 or page_table.shape[0] != kv_len.shape[0]:
+        raise ValueError("page_table and kv_len hold one int32 row and one int32 per sequence")
+    c.n_pages, c.n_kv_heads, c.page_size, c.head_dim = (int(n) for n in K.shape)
+    c.dtype, c.max_pages = dtype, int(page_table.shape[1])
+    c.K, c.V, c.page_table, c.kv_len = _ptr(K), _ptr(V), _ptr(page_table), _ptr(kv_len)
+    c.host_page_table, c.host_kv_len = _ptr(host_page_table), _ptr(host_kv_len)
+    c._keep = (K, V, page_table, kv_len, host_page_table, host_kv_len)
+    return c
+
+
+def zo_cache_append(batch, Q, ldq, K, ldk, V, ldv, n_heads, gamma_q, gamma_k, norm_eps, rope_theta, cache, Qout, ldqo,
+                    stream=None):
+    _check(lib().zo_cache_append(C.byref(batch), _ptr(Q), ldq, _ptr(K), ldk, _ptr(V), ldv, n_heads, _ptr(gamma_q),
+                                 _ptr(gamma_k), norm_eps, rope_theta, C.byref(cache), _ptr(Qout), ldqo, _stream(stream)))
+
+
+def zo_attention_paged_workspace_bytes(n_tokens, n_heads, head_dim, max_len, dtype):
+    return lib().zo_attention_paged_workspace_bytes(n_tokens, n_heads, head_dim, max_len, dtype)
+
+
+def zo_attention_paged(batch, Q, ldq, n_heads, scale, cache, O, ldo, workspace, workspace_bytes, stream=None):
+    _check(lib().zo_attention_paged(C.byref(batch), _ptr(Q), ldq, n_heads, scale, C.byref(cache), _ptr(O), ldo,
+                                    _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def zo_sample_workspace_bytes(n_rows, vocab, dtype):
+    return lib().zo_sample_workspace_bytes(n_rows, vocab, dtype)
+
+
+def zo_sample(logits, ld, n_rows, vocab, dtype, temperature, top_k, top_p, min_p, u, tokens, prob, n_kept, workspace,
+              workspace_bytes, stream=None):
+    _check(lib().zo_sample(_ptr(logits), ld, n_rows, vocab, dtype, _ptr(temperature), _ptr(top_k), _ptr(top_p),
+                           _ptr(min_p), _ptr(u), _ptr(tokens), _ptr(prob), _ptr(n_kept), _ptr(workspace),
+                           workspace_bytes, _stream(stream)))
+
+
+def zo_embed_rows(tokens, pos, n_rows, E, lde, vocab, E_pos, ldp, n_pos, d, dtype, X, ldx, pos_next, stream=None):
+    _check(lib().zo_embed_rows(_ptr(tokens), _ptr(pos), n_rows, _ptr(E), lde, vocab, _ptr(E_pos), ldp, n_pos, d, dtype,
+                               _ptr(X), ldx, _ptr(pos_next), _stream(stream)))
 
 
 def make_layer_banks(entries):

@@ -448,6 +448,10 @@ int32_t zo::score_validate(const zo_batch* batch, const void* H, int64_t ldh, co
 }
 
 int32_t zo::fail_status(int32_t status, const char* message) { return fail((zo_status)status, "%s", message); }
+int32_t zo::batch_validate(const zo_batch* batch) { return check_batch(batch); }
+int32_t zo::matrix_validate(const char* name, const void* p, int64_t ld, int cols, zo_dtype dtype) {
+  return check_matrix(name, p, ld, cols, dtype);
+}
 
 extern "C" {
 

@@ -299,4 +299,55 @@ int attention_f32_max_head_dim();
 int attention_bf16_head_dim();
 hipError_t launch_attention(const AttnArgs& a, hipStream_t st);
 
+// ---- zo_cache.hip (decoding: the paged cache) ------------------------------------------------
+struct CacheDev {
+  void* K; void* V;                 // [n_pages][n_kv_heads][page_size][dh]
+  const int32_t* table;             // [S][max_pages]
+  const int32_t* kv_len;            // [S]
+  int n_pages, page_shift, max_pages;
+  int n_kv_heads, dh, bf16;
+};
+struct AppendArgs {
+  const void* Q; int64_t ldq;       // [T][n_heads * dh]
+  const void* K; int64_t ldk;       // [T][n_kv_heads * dh]
+  const void* V; int64_t ldv;
+  void* Qout; int64_t ldqo;         // may be Q
+  const int32_t* cu; int S, T;
+  int n_heads;
+  const float* gamma_q; const float* gamma_k;   // both null: no norm
+  float eps;
+  float theta;                      // <= 0: no rotation
+  CacheDev c;
+};
+hipError_t launch_cache_append(const AppendArgs& a, hipStream_t st);
+
+struct PagedAttnArgs {
+  const void* Q; int64_t ldq;       // [T][n_heads * dh]
+  void* O; int64_t ldo;
+  const int32_t* cu; int S, T;
+  int n_heads, group;               // group = n_heads / n_kv_heads
+  float scale;
+  CacheDev c;
+};
+hipError_t launch_attention_paged(const PagedAttnArgs& a, hipStream_t st);
+
+// ---- zo_sample.hip -------------------------------------------------------------------------------
+struct SampleArgs {
+  const void* z; int64_t ld;        // [T][V]
+  int T, V, bf16;
+  const float* temperature; const int32_t* top_k; const float* top_p; const float* min_p; const float* u;
+  int32_t* tokens; float* prob; int32_t* n_kept;
+};
+hipError_t launch_sample(const SampleArgs& a, hipStream_t st);
+
+struct EmbedArgs {
+  const int32_t* tokens; const int32_t* pos; int T;
+  const void* E; int64_t lde; int vocab;
+  const void* Epos; int64_t ldp; int n_pos;
+  int d, bf16;
+  void* X; int64_t ldx;
+  int32_t* pos_next;
+};
+hipError_t launch_embed_rows(const EmbedArgs& a, hipStream_t st);
+
 }  // namespace zo
