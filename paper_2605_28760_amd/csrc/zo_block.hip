@@ -360,15 +360,6 @@ __device__ __forceinline__ bool find_query_block(const int32_t* cu, int S, int w
 // to 30 rows, 40 heads: 50 -> 40; the 32-key form above, three per unit, 28).  Three waves per SIMD with 64 keys (168
 // registers, one stage of keys or values, a second barrier per step) spill and take 440 to 490 us, and 35 on the short.
 
-// Largest of the four lanes l, l ^ 16, l ^ 32, l ^ 48 (the lanes that share a query), in the vector ALU.
-__device__ __forceinline__ float column_max(float x) {
-  const uint32_t u = __float_as_uint(x);
-  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-  const uint32_t v = __float_as_uint(fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1])));
-  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
-
 __global__ __launch_bounds__(kAttnWaves* kWave, 2) void k_attention_bf16(AttnArgs a) {
   // [2] stages of keys, [2] stages of values.  (Dynamic: with named arrays the compiler tracks which of them a
   // direct-to-LDS load writes and waits for the next step's loads before it reads this step's stage.)

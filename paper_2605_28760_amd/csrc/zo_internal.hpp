@@ -328,7 +328,11 @@ struct PagedAttnArgs {
   int n_heads, group;               // group = n_heads / n_kv_heads
   float scale;
   CacheDev c;
+  int ranges;                       // ranges of a row that the workspace has room for (attention_paged_ranges)
+  float* part_ml;                   // [T][n_heads][ranges][2] maximum and sum (null when ranges == 1)
+  float* part_o;                    // [T][n_heads][ranges][dh]
 };
+int attention_paged_ranges(int max_len);   // most ranges of a row of up to max_len positions
 hipError_t launch_attention_paged(const PagedAttnArgs& a, hipStream_t st);
 
 // ---- zo_sample.hip -------------------------------------------------------------------------------
