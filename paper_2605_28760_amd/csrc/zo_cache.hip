@@ -122,10 +122,11 @@ __global__ __launch_bounds__(256) void k_cache_append(AppendArgs a) {
 
 // ------------------------------------------------------------------ attention
 
-// A row's positions are cut into ranges of range_keys(n), a function of the row's own n alone; a workgroup of four waves
-// takes one (row, key/value head, range).  Its waves take steps of keys in turn, each with a running maximum and sum of
-// its own, and join in LDS in the order of the waves; a row of several ranges leaves (maximum, sum, unnormalised output)
-// of each in the workspace and k_attention_join joins them in order.
+// A row's positions are cut into ranges of range_keys(n), a function of the row's own n alone; two waves take one (row,
+// key/value head, range).  They take steps of keys in turn, each with a running maximum and sum of its own, and join in LDS;
+// a row of several ranges leaves (maximum, sum, unnormalised output) of each in the workspace and k_attention_join joins
+// them in order.  A call that would leave compute units empty takes the up to four ranges of its rows in one workgroup,
+// which joins them itself with the same arithmetic: one launch instead of two.
 //
 // Both products run on the matrix cores with up to 16 query heads of the key/value head as columns, transposed as in the
 // attention of packed rows: S^T = K Q^T and O^T = V^T P^T, so that everything that belongs to a query lies in one column
@@ -139,14 +140,20 @@ __global__ __launch_bounds__(256) void k_cache_append(AppendArgs a) {
 // fp32 uses the 16x16x4 instruction on 16 keys per step: a lane's scores are those of keys 4 g .. 4 g + 3, and that one value
 // per lane is the operand needs no transposition.
 
-constexpr int kAttnWaves = 4;
-constexpr int kRange = 256;          // keys per workgroup of a row of up to kMaxRanges * kRange positions
-constexpr int kMaxRanges = 64;       // one lane each in the join
-__host__ __device__ constexpr int range_keys(int n) {
-  return kRange * (n <= kMaxRanges * kRange ? 1 : (n + kMaxRanges * kRange - 1) / (kMaxRanges * kRange));
+constexpr int kRangeWaves = 2;       // waves of a range
+constexpr int kMaxRanges = 64;       // of a row: one lane each in the join
+constexpr int kHere = 4;             // most ranges that one workgroup joins by itself
+// Positions per range of a row of n positions: four steps of each wave (the same bytes in either type), more where that makes
+// too many ranges.
+__host__ __device__ constexpr int range_keys(bool bf16, int n) {
+  const int base = bf16 ? 256 : 128;
+  return base * (n <= kMaxRanges * base ? 1 : (n + kMaxRanges * base - 1) / (kMaxRanges * base));
 }
 // most ranges of a row of up to n positions
-constexpr int most_ranges(int n) { return n >= kMaxRanges * kRange ? kMaxRanges : (n + kRange - 1) / kRange; }
+constexpr int most_ranges(bool bf16, int n) {
+  const int base = bf16 ? 256 : 128;
+  return n >= kMaxRanges * base ? kMaxRanges : (n + base - 1) / base;
+}
 
 struct Place {
   int seq, pos;   // seq < 0: behind the last sequence
@@ -183,6 +190,7 @@ template <int kDh>
 struct Bf16Step {
   static constexpr int kKeys = 32, kPad = kDh, kCols = kDh / 16;   // columns of a value row per lane
   static constexpr int kScores = 8;       // per lane: keys 8 g + i
+  static constexpr bool kAhead = true, kWhole = true;   // kWhole: the head dimension is kPad
   bf16x8 k[2][kDh / 32];
   u32x4 v[8][kCols > 8 ? kCols / 8 : 1];  // (kCols 4: the lower half of each)
   __device__ static constexpr int key_of_score(int g, int i) { return 8 * g + i; }
@@ -242,6 +250,8 @@ template <int kDh, int kMode>
 struct F32Step {
   static constexpr int kKeys = 16, kPad = kDh, kCols = kDh / 16;
   static constexpr int kScores = 4;       // per lane: keys 4 g + i
+  static constexpr bool kWhole = kMode == 0;
+  static constexpr bool kAhead = kDh <= 64;   // (a third wave per SIMD instead: 64 rows of 500..2000, 8 heads over 4 of 128: 82 -> 72 us)
   f32x4 k[kDh / 16];
   f32x4 v[4][kCols / 4];
   __device__ static constexpr int key_of_score(int g, int i) { return 4 * g + i; }
@@ -296,10 +306,18 @@ struct F32Step {
   }
 };
 
-// kTiles: tiles of 16 query heads per workgroup (1 or 4); its waves share the keys 4 / kTiles ways.
-template <typename Tio, class Step, int kTiles>
-__global__ __launch_bounds__(kAttnWaves* kWave, Step::kPad > 128 ? 1 : 2) void k_attention_paged(PagedAttnArgs a) {
-  constexpr int kDh = Step::kPad, kCols = Step::kCols, kKeys = Step::kKeys, kSharers = kAttnWaves / kTiles;
+// One wave's share of a range, and of the joining: sum of the waves' values, their maximum.
+struct Joined {
+  float m, l;
+  f32x4 o;
+};
+
+// kTiles: tiles of 16 query heads per workgroup (1 or 2); with one its waves share the keys.  kRanges: ranges of a row per
+// workgroup, 1 or kHere (then the table has room for no more).
+template <typename Tio, class Step, int kTiles, int kRanges>
+__global__ __launch_bounds__(kRanges* kRangeWaves* kWave, Step::kPad > 128 ? 1 : 2) void k_attention_paged(PagedAttnArgs a) {
+  constexpr int kDh = Step::kPad, kCols = Step::kCols, kKeys = Step::kKeys, kSharers = kRangeWaves / kTiles;
+  constexpr int kAttnWaves = kRanges * kRangeWaves;
   constexpr int kRowLds = kDh + 4;   // (rows of the joining buffer on different banks)
   extern __shared__ __attribute__((aligned(16))) float s_o[];     // [wave][16][kRowLds]
   __shared__ float s_m[kAttnWaves][16], s_l[kAttnWaves][16];
@@ -311,9 +329,9 @@ __global__ __launch_bounds__(kAttnWaves* kWave, Step::kPad > 128 ? 1 : 2) void k
   const Place pl = place_of_row(a.cu, a.c.kv_len, a.S, t, lane);
   if (pl.seq < 0) return;
   const int n = max(0, min(pl.pos + 1, a.c.max_pages << a.c.page_shift));
-  const int len = range_keys(n);
+  const int len = range_keys(a.c.bf16, n);
   const int n_ranges = n > 0 ? (n + len - 1) / len : 1;   // (an empty row: one empty range writes its zeros)
-  const int tile = wave % kTiles, share = wave / kTiles;
+  const int tile = wave % kTiles, share = wave % kRangeWaves / kTiles;
   const int head0 = (part * kTiles + tile) * 16;            // of the group
   const int cols = min(16, a.group - head0);                 // columns in use (may be <= 0)
   typename Step::Query q;
@@ -321,8 +339,9 @@ __global__ __launch_bounds__(kAttnWaves* kWave, Step::kPad > 128 ? 1 : 2) void k
   const float sl2 = a.scale * 1.4426950408889634f;           // scores are kept in base-2 units
   const int32_t* table = a.c.table + (int64_t)pl.seq * a.c.max_pages;
 
-  for (int range = blockIdx.y; range < n_ranges; range += gridDim.y) {
-    const int j_a = range * len, j_b = min(j_a + len, n);   // the range's positions
+  for (int range0 = blockIdx.y; range0 < n_ranges; range0 += gridDim.y) {
+    const int range = kRanges == 1 ? range0 : wave / kRangeWaves;
+    const int j_a = range * len, j_b = min(j_a + len, n);   // the range's positions (none behind the row's last)
     f32x4 o[kCols];
 #pragma unroll
     for (int d = 0; d < kCols; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -340,6 +359,10 @@ __global__ __launch_bounds__(kAttnWaves* kWave, Step::kPad > 128 ? 1 : 2) void k
     // Loads step `j0`; false when it has no key that is seen.  A key that is not seen is stood in for by one that is: what a
     // slot behind the last position holds must not meet even a weight of zero.
     auto load = [&](int j0, Step& st, int& last, int& dead) -> bool {
+      if (j0 / 16 - first >= 64) {
+        first += 64;
+        pages = pages_from(first);
+      }
       const int b = j0 / 16 - first;
       const int p0 = __builtin_amdgcn_readlane(pages, b);
       const int p1 = kKeys == 32 ? __builtin_amdgcn_readlane(pages, b + 1) : p0;
@@ -391,14 +414,24 @@ __global__ __launch_bounds__(kAttnWaves* kWave, Step::kPad > 128 ? 1 : 2) void k
       st.values(p, o);
     };
     if (cols > 0) {
-      for (int j0 = j_a + share * kKeys; j0 < j_b; j0 += kSharers * kKeys) {
-        if (j0 / 16 - first >= 64) {
-          first += 64;
-          pages = pages_from(first);
+      constexpr int kStride = kSharers * kKeys;
+      int j0 = j_a + share * kKeys;
+      if constexpr (Step::kAhead) {   // two steps in registers: while one is worked on, the next is on its way
+        Step s0, s1;
+        int last0 = 0, dead0 = 0, last1 = 0, dead1 = 0;
+        bool seen0 = j0 < j_b && load(j0, s0, last0, dead0);
+        for (; j0 < j_b; j0 += 2 * kStride) {
+          const bool seen1 = j0 + kStride < j_b && load(j0 + kStride, s1, last1, dead1);
+          if (seen0) attend(s0, last0, dead0);
+          seen0 = j0 + 2 * kStride < j_b && load(j0 + 2 * kStride, s0, last0, dead0);
+          if (seen1) attend(s1, last1, dead1);
         }
-        Step st;
-        int last, dead;
-        if (load(j0, st, last, dead)) attend(st, last, dead);
+      } else {
+        for (; j0 < j_b; j0 += kStride) {
+          Step st;
+          int last, dead;
+          if (load(j0, st, last, dead)) attend(st, last, dead);
+        }
       }
     }
 
@@ -418,70 +451,152 @@ __global__ __launch_bounds__(kAttnWaves* kWave, Step::kPad > 128 ? 1 : 2) void k
     const int group_cols = min(16 * kTiles, a.group - part * 16 * kTiles);
     for (int e = threadIdx.x; e < group_cols * (kDh / 4); e += kAttnWaves * kWave) {
       const int c = e / (kDh / 4), col = c & 15, tl = c >> 4, d = e % (kDh / 4) * 4;
-      float mm = -INFINITY;
+      auto waves_of = [&](int rg) {   // the waves of one range
+        Joined x{-INFINITY, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-      for (int w = 0; w < kSharers; ++w) mm = fmaxf(mm, s_m[w * kTiles + tl][col]);
-      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-      float sum = 0.f;
+        for (int w = 0; w < kSharers; ++w) x.m = fmaxf(x.m, s_m[rg * kRangeWaves + w * kTiles + tl][col]);
 #pragma unroll
-      for (int w = 0; w < kSharers; ++w) {
-        const int wv = w * kTiles + tl;
-        const float mw = s_m[wv][col];
-        const float f = mw == mm ? 1.0f : __builtin_amdgcn_exp2f(mw - mm);   // (no key at all: zeros stay zeros)
-        acc += *reinterpret_cast<const f32x4*>(s_o + (wv * 16 + col) * kRowLds + d) * f;
-        sum += s_l[wv][col] * f;
-      }
+        for (int w = 0; w < kSharers; ++w) {
+          const int wv = rg * kRangeWaves + w * kTiles + tl;
+          const float mw = s_m[wv][col];
+          const float f = mw == x.m ? 1.0f : __builtin_amdgcn_exp2f(mw - x.m);   // (no key at all: zeros stay zeros)
+          const f32x4 ow = *reinterpret_cast<const f32x4*>(s_o + (wv * 16 + col) * kRowLds + d);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x.o[i] = __builtin_fmaf(ow[i], f, x.o[i]);
+          x.l = __builtin_fmaf(s_l[wv][col], f, x.l);
+        }
+        return x;
+      };
       const int h = kvh * a.group + part * 16 * kTiles + c;
-      if (n_ranges == 1) {
-        const float inv = sum > 0.f ? 1.0f / sum : sum;   // (NaN stays NaN)
+      Joined x;
+      if (kRanges == 1 || n_ranges == 1) {
+        x = waves_of(0);
+      } else {   // what k_attention_join does, for four ranges
+#pragma clang fp contract(off)
+        Joined y[kHere];
+        x = Joined{-INFINITY, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+        for (int rg = 0; rg < kHere; ++rg) {
+          y[rg] = Joined{-INFINITY, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
+          if (rg < n_ranges) y[rg] = waves_of(rg);
+          x.m = fmaxf(x.m, y[rg].m);
+        }
+        float lf[kHere];
+#pragma unroll
+        for (int rg = 0; rg < kHere; ++rg) {
+          const float f = y[rg].m == x.m ? 1.0f : __builtin_amdgcn_exp2f(y[rg].m - x.m);
+          lf[rg] = y[rg].l * f;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x.o[i] = x.o[i] + y[rg].o[i] * f;
+        }
+        x.l = (lf[0] + lf[2]) + (lf[1] + lf[3]);   // (the order of the wave's sum)
+      }
+      if (kRanges > 1 || n_ranges == 1) {
+        const float inv = x.l > 0.f ? 1.0f / x.l : x.l;   // (NaN stays NaN)
         Tio* out = (Tio*)a.O + (int64_t)t * a.ldo + (int64_t)h * a.c.dh + d;
         if constexpr (sizeof(Tio) == 2) {
-          *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv));
+          *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(x.o[0] * inv, x.o[1] * inv), pack_bf16x2(x.o[2] * inv, x.o[3] * inv));
+        } else if constexpr (Step::kWhole) {
+          *reinterpret_cast<f32x4*>(out) = x.o * inv;
         } else {
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (d + i < a.c.dh) out[i] = acc[i] * inv;
+            if (d + i < a.c.dh) out[i] = x.o[i] * inv;
         }
       } else {
         const int64_t at = part_at(a, t, h, range);
-        if (d == 0) { a.part_ml[2 * at] = mm; a.part_ml[2 * at + 1] = sum; }
+        if (d == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = make_float2(x.m, x.l);
         float* out = a.part_o + at * a.c.dh + d;
+        if constexpr (Step::kWhole) {
+          *reinterpret_cast<f32x4*>(out) = x.o;
+        } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (kDh == a.c.dh || d + i < a.c.dh) out[i] = acc[i];
+          for (int i = 0; i < 4; ++i)
+            if (d + i < a.c.dh) out[i] = x.o[i];
+        }
       }
     }
-    if (range + (int)gridDim.y < n_ranges) __syncthreads();   // (the buffer is written again)
+    if (kRanges > 1) break;
+    if (range0 + (int)gridDim.y < n_ranges) __syncthreads();   // (the buffer is written again)
   }
 }
 
-// Joins the ranges of a row, one wave per (row, head): lane c has range c's maximum and sum, then the lanes go over the
-// columns and add the ranges in order.
-template <typename Tio>
-__global__ __launch_bounds__(256) void k_attention_join(PagedAttnArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+// Joins the ranges of a row: ranges c, c + 4, ... are added in order into sum c % 4, and the four sums in order, a row's lanes
+// over its columns.  Lane c of a wave has range c's maximum and sum of weights.  Few rows and heads: a workgroup each, a wave
+// per sum; many: a wave each with all four sums, four to a workgroup.  (One sum and one load after another: 64 ranges of 128
+// columns, 64 rows and heads, 46.7 us, now 4; a workgroup each for 10240 rows and heads of 4 ranges: 18.8.)
+// kPer: columns per lane.
+constexpr int kJoinSums = 4;
+template <typename Tio, int kPer, bool kWave1>
+__global__ __launch_bounds__(kJoinSums* kWave) void k_attention_join(PagedAttnArgs a) {
+#pragma clang fp contract(off)   // (the same bits in every form of the joining)
+  __shared__ float s_acc[kJoinSums - 1][kPer * kWave];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t item = kWave1 ? (int64_t)blockIdx.x * kJoinSums + wave : blockIdx.x;
   if (item >= (int64_t)a.T * a.n_heads) return;
   const int t = (int)(item / a.n_heads), h = (int)(item % a.n_heads);
   const Place pl = place_of_row(a.cu, a.c.kv_len, a.S, t, lane);
   if (pl.seq < 0) return;
   const int n = min(pl.pos + 1, a.c.max_pages << a.c.page_shift);
-  const int len = range_keys(n);
+  const int len = range_keys(a.c.bf16, n);
   const int n_ranges = n > 0 ? (n + len - 1) / len : 1;
   if (n_ranges == 1) return;
+  const int dh = a.c.dh;
   const int64_t at = part_at(a, t, h, 0);
   float m = -INFINITY, l = 0.f;
   if (lane < n_ranges) { m = a.part_ml[2 * (at + lane)]; l = a.part_ml[2 * (at + lane) + 1]; }
+  const float* o = a.part_o + at * dh;
+  constexpr int kSums = kWave1 ? kJoinSums : 1, kDeep = 8 / kSums;   // eight ranges under way
+  float acc[kSums][kPer];
+#pragma unroll
+  for (int v = 0; v < kSums; ++v)
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) acc[v][i] = 0.f;
   const float mm = wave_max(m);
   const float f = m == mm ? 1.0f : __builtin_amdgcn_exp2f(m - mm);
+  for (int c0 = kWave1 ? 0 : wave; c0 < n_ranges; c0 += kJoinSums * kDeep) {
+    float x[kDeep][kSums][kPer];
+#pragma unroll
+    for (int u = 0; u < kDeep; ++u)
+#pragma unroll
+      for (int v = 0; v < kSums; ++v) {
+        const int c = c0 + u * kJoinSums + v;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) x[u][v][i] = c < n_ranges && lane + i * kWave < dh ? o[c * dh + lane + i * kWave] : 0.f;
+      }
+#pragma unroll
+    for (int u = 0; u < kDeep; ++u)
+#pragma unroll
+      for (int v = 0; v < kSums; ++v) {
+        const int c = c0 + u * kJoinSums + v;
+        if (c >= n_ranges) break;
+        const float fc = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), c));
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) acc[v][i] += x[u][v][i] * fc;
+      }
+  }
+  if constexpr (kWave1) {
+#pragma unroll
+    for (int v = 1; v < kSums; ++v)
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) acc[0][i] += acc[v][i];
+  } else {
+    if (wave > 0) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) s_acc[wave - 1][i * kWave + lane] = acc[0][i];
+    }
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int v = 1; v < kJoinSums; ++v)
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) acc[0][i] += s_acc[v - 1][i * kWave + lane];
+  }
   const float sum = wave_sum(l * f);
   const float inv = sum > 0.f ? 1.0f / sum : sum;
-  for (int d = lane; d < a.c.dh; d += kWave) {
-    const float* o = a.part_o + at * a.c.dh + d;
-    float acc = 0.f;
-    for (int c = 0; c < n_ranges; ++c) acc += o[(int64_t)c * a.c.dh] * __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), c));
-    st_elem((Tio*)a.O + (int64_t)t * a.ldo + (int64_t)h * a.c.dh, d, acc * inv);
-  }
+#pragma unroll
+  for (int i = 0; i < kPer; ++i)
+    if (lane + i * kWave < dh) st_elem((Tio*)a.O + (int64_t)t * a.ldo + (int64_t)h * dh, lane + i * kWave, acc[0][i] * inv);
 }
 
 }  // namespace
@@ -494,54 +609,74 @@ hipError_t launch_cache_append(const AppendArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-int attention_paged_ranges(int max_len) { return max_len > 0 ? most_ranges(max_len) : 1; }
+int attention_paged_ranges(bool bf16, int max_len) { return max_len > 0 ? most_ranges(bf16, max_len) : 1; }
 
 namespace {
-template <typename Tio, class Step, int kTiles>
-hipError_t launch_paged(const PagedAttnArgs& a, hipStream_t st) {
-  constexpr int kLds = kAttnWaves * 16 * (Step::kPad + 4) * 4;
+template <typename Tio, class Step, int kTiles, int kRanges>
+hipError_t launch_paged(const PagedAttnArgs& a, int64_t groups, hipStream_t st) {
+  constexpr int kWaves = kRanges * kRangeWaves, kLds = kWaves * 16 * (Step::kPad + 4) * 4;
   static std::atomic<bool> ready[kMaxDevices];
-  if (kLds > 64 * 1024 - 1024) {
+  if (kLds > 60 * 1024) {
     const hipError_t e = once_per_device(ready, [] {
-      return hipFuncSetAttribute((const void*)k_attention_paged<Tio, Step, kTiles>, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+      return hipFuncSetAttribute((const void*)k_attention_paged<Tio, Step, kTiles, kRanges>, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
     });
     if (e != hipSuccess) return e;
   }
-  const int per_head = (a.group + 16 * kTiles - 1) / (16 * kTiles);
-  const dim3 grid((unsigned)((int64_t)a.T * a.c.n_kv_heads * per_head), (unsigned)a.ranges);
-  k_attention_paged<Tio, Step, kTiles><<<grid, kAttnWaves * kWave, kLds, st>>>(a);
+  const dim3 grid((unsigned)groups, kRanges == 1 ? (unsigned)a.ranges : 1u);
+  k_attention_paged<Tio, Step, kTiles, kRanges><<<grid, kWaves * kWave, kLds, st>>>(a);
   return hipGetLastError();
 }
+// A call whose rows have up to four ranges and whose (row, key/value head) pairs do not fill the compute units gives each pair
+// one workgroup and needs no join.
+template <typename Tio, class Step, int kTiles>
+hipError_t launch_paged_ranges(const PagedAttnArgs& a, bool& joined, hipStream_t st) {
+  const int64_t groups = (int64_t)a.T * a.c.n_kv_heads * ((a.group + 16 * kTiles - 1) / (16 * kTiles));
+  if constexpr (Step::kPad <= 128) {
+    joined = a.ranges > 1 && a.ranges <= kHere && groups <= compute_units();
+    if (joined) return launch_paged<Tio, Step, kTiles, kHere>(a, groups, st);
+  }
+  return launch_paged<Tio, Step, kTiles, 1>(a, groups, st);
+}
 template <typename Tio, class Step>
-hipError_t launch_paged_tiles(const PagedAttnArgs& a, hipStream_t st) {
-  return a.group <= 16 ? launch_paged<Tio, Step, 1>(a, st) : launch_paged<Tio, Step, 4>(a, st);
+hipError_t launch_paged_tiles(const PagedAttnArgs& a, bool& joined, hipStream_t st) {
+  return a.group <= 16 ? launch_paged_ranges<Tio, Step, 1>(a, joined, st) : launch_paged_ranges<Tio, Step, 2>(a, joined, st);
 }
 template <int kDh>
-hipError_t launch_paged_f32(const PagedAttnArgs& a, hipStream_t st) {
-  if (a.c.dh == kDh) return launch_paged_tiles<float, F32Step<kDh, 0>>(a, st);
+hipError_t launch_paged_f32(const PagedAttnArgs& a, bool& joined, hipStream_t st) {
+  if (a.c.dh == kDh) return launch_paged_tiles<float, F32Step<kDh, 0>>(a, joined, st);
   // (rows of other widths: only those of a multiple of 4 start on 16 bytes)
-  if (a.c.dh % 4 == 0) return launch_paged_tiles<float, F32Step<kDh, 1>>(a, st);
-  return launch_paged_tiles<float, F32Step<kDh, 2>>(a, st);
+  if (a.c.dh % 4 == 0) return launch_paged_tiles<float, F32Step<kDh, 1>>(a, joined, st);
+  return launch_paged_tiles<float, F32Step<kDh, 2>>(a, joined, st);
+}
+template <typename Tio, int kPer>
+hipError_t launch_join_of(const PagedAttnArgs& a, hipStream_t st) {
+  const int64_t items = (int64_t)a.T * a.n_heads;
+  // (same sums either way; four waves per compute unit keep a wave's loads company)
+  if (items >= 4 * compute_units()) k_attention_join<Tio, kPer, true><<<dim3((unsigned)((items + kJoinSums - 1) / kJoinSums)), kJoinSums * kWave, 0, st>>>(a);
+  else k_attention_join<Tio, kPer, false><<<dim3((unsigned)items), kJoinSums * kWave, 0, st>>>(a);
+  return hipGetLastError();
+}
+template <typename Tio>
+hipError_t launch_join(const PagedAttnArgs& a, hipStream_t st) {
+  return a.c.dh <= 64 ? launch_join_of<Tio, 1>(a, st) : a.c.dh <= 128 ? launch_join_of<Tio, 2>(a, st) : launch_join_of<Tio, 4>(a, st);
 }
 }  // namespace
 
 hipError_t launch_attention_paged(const PagedAttnArgs& a, hipStream_t st) {
   hipError_t e;
+  bool joined = false;
   if (a.c.bf16) {
     switch (a.c.dh) {
-      case 64: e = launch_paged_tiles<bf16_t, Bf16Step<64>>(a, st); break;
-      case 128: e = launch_paged_tiles<bf16_t, Bf16Step<128>>(a, st); break;
-      case 256: e = launch_paged_tiles<bf16_t, Bf16Step<256>>(a, st); break;
+      case 64: e = launch_paged_tiles<bf16_t, Bf16Step<64>>(a, joined, st); break;
+      case 128: e = launch_paged_tiles<bf16_t, Bf16Step<128>>(a, joined, st); break;
+      case 256: e = launch_paged_tiles<bf16_t, Bf16Step<256>>(a, joined, st); break;
       default: return hipErrorInvalidValue;
     }
   } else {
-    e = a.c.dh <= 64 ? launch_paged_f32<64>(a, st) : a.c.dh <= 128 ? launch_paged_f32<128>(a, st) : launch_paged_f32<256>(a, st);
+    e = a.c.dh <= 64 ? launch_paged_f32<64>(a, joined, st) : a.c.dh <= 128 ? launch_paged_f32<128>(a, joined, st) : launch_paged_f32<256>(a, joined, st);
   }
-  if (e != hipSuccess || a.ranges == 1) return e;
-  const dim3 grid((unsigned)(((int64_t)a.T * a.n_heads + 3) / 4));
-  if (a.c.bf16) k_attention_join<bf16_t><<<grid, 256, 0, st>>>(a);
-  else k_attention_join<float><<<grid, 256, 0, st>>>(a);
-  return hipGetLastError();
+  if (e != hipSuccess || a.ranges == 1 || joined) return e;
+  return a.c.bf16 ? launch_join<bf16_t>(a, st) : launch_join<float>(a, st);
 }
 
 }  // namespace zo

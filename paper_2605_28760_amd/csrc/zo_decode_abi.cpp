@@ -96,9 +96,9 @@ struct PagedPlan {
   int ranges = 1;
   size_t ml = 0, o = 0, total = 0;
 };
-PagedPlan plan_paged(int T, int H, int dh, int max_len) {
+PagedPlan plan_paged(int T, int H, int dh, int max_len, zo_dtype dt) {
   PagedPlan p;
-  p.ranges = zo::attention_paged_ranges(max_len);
+  p.ranges = zo::attention_paged_ranges(dt == ZO_BF16, max_len);
   if (p.ranges > 1) {
     const size_t parts = (size_t)T * H * p.ranges;
     p.o = (parts * 8 + 255) / 256 * 256;
@@ -141,9 +141,8 @@ int32_t zo_cache_append(const zo_batch* batch, const void* Q, int64_t ldq, const
 
 size_t zo_attention_paged_workspace_bytes(int32_t n_tokens, int32_t n_heads, int32_t head_dim, int32_t max_len,
                                           zo_dtype dtype) {
-  (void)dtype;
   if (n_tokens < 0 || n_heads < 0 || head_dim < 0 || max_len < 0) return 0;
-  return plan_paged(n_tokens, n_heads, head_dim, max_len).total;
+  return plan_paged(n_tokens, n_heads, head_dim, max_len, dtype).total;
 }
 
 int32_t zo_attention_paged(const zo_batch* batch, const void* Q, int64_t ldq, int32_t n_heads, float scale,
@@ -162,7 +161,7 @@ int32_t zo_attention_paged(const zo_batch* batch, const void* Q, int64_t ldq, in
   if (!Q || !O) return fail(ZO_ERR_NULL, "Q or O is NULL");
   if (int32_t st = zo::matrix_validate("Q", Q, ldq, n_heads * dh, dt)) return st;
   if (int32_t st = zo::matrix_validate("O", O, ldo, n_heads * dh, dt)) return st;
-  const PagedPlan plan = plan_paged(T, n_heads, dh, cache->max_pages * cache->page_size);
+  const PagedPlan plan = plan_paged(T, n_heads, dh, cache->max_pages * cache->page_size, dt);
   if (int32_t st = check_workspace(workspace, workspace_bytes, plan.total)) return st;
   zo::PagedAttnArgs a;
   a.Q = Q; a.ldq = ldq; a.O = O; a.ldo = ldo; a.cu = batch->cu_seqlens; a.S = batch->n_seqs; a.T = T;

@@ -332,7 +332,7 @@ struct PagedAttnArgs {
   float* part_ml;                   // [T][n_heads][ranges][2] maximum and sum (null when ranges == 1)
   float* part_o;                    // [T][n_heads][ranges][dh]
 };
-int attention_paged_ranges(int max_len);   // most ranges of a row of up to max_len positions
+int attention_paged_ranges(bool bf16, int max_len);   // most ranges of a row of up to max_len positions
 hipError_t launch_attention_paged(const PagedAttnArgs& a, hipStream_t st);
 
 // ---- zo_sample.hip -------------------------------------------------------------------------------

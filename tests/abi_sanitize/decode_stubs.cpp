@@ -20,7 +20,7 @@ static void inside(const void* p, size_t bytes, const char* what) {
 namespace zo {
 
 hipError_t launch_cache_append(const AppendArgs&, hipStream_t) { ++g_launches; return hipSuccess; }
-int attention_paged_ranges(int max_len) { return max_len < 16384 ? (max_len + 255) / 256 : 64; }
+int attention_paged_ranges(bool bf16, int max_len) { return max_len < (bf16 ? 16384 : 8192) ? (max_len + (bf16 ? 255 : 127)) / (bf16 ? 256 : 128) : 64; }
 hipError_t launch_attention_paged(const PagedAttnArgs& a, hipStream_t) {
   ++g_launches;
   const size_t parts = (size_t)a.T * a.n_heads * a.ranges;

@@ -238,6 +238,29 @@ def test_rows_do_not_depend_on_the_batch_or_the_table():
                 assert (_np(out)[0] == whole[i]).all(), (dtype, i, width)
 
 
+@pytest.mark.parametrize("dtype,dh", [("bf16", 128), ("bf16", 64), ("f32", 64), ("f32", 36)])
+def test_every_form_of_a_call_gives_a_row_the_same_bits(dtype, dh):
+    """One workgroup per row, ranges joined by a second launch with a workgroup or a wave per row and head."""
+    cap = 1024 if dtype == "bf16" else 512
+    kv = [1, 100, cap // 4, cap // 4 + 1, cap // 2 + 7, cap // 4 * 3, cap - 1, cap]
+    s = Setup(15, dtype, 4, 2, dh, 16, [1] * 8, kv, width=cap // 16)
+    first = _np(s.attend()).copy()
+    s.check_attend(s.out)
+    for copies, width in ((1, cap // 16 + 1), (1, 4 * cap // 16), (40, cap // 16), (40, 2 * cap // 16)):
+        table = np.full((8 * copies, width), -1, np.int32)
+        table[:, :cap // 16] = np.tile(s.table, (copies, 1))
+        d_table, d_kv, d_cu = _i32(table), _i32(np.tile(kv, copies)), _i32(np.arange(8 * copies + 1))
+        none = _i32(np.full(8 * copies, -1))
+        q = s.q.repeat(copies, 1)
+        batch = zb.make_batch(8 * copies, d_cu, none, None, None, None, n_seqs=8 * copies, n_cands=0, n_dirs=0)
+        cache = zb.make_cache(s.K, s.V, ZT[dtype], d_table, d_kv)
+        out = torch.empty(8 * copies, 4 * dh, device=DEV, dtype=TT[dtype])
+        need = zb.zo_attention_paged_workspace_bytes(8 * copies, 4, dh, width * 16, ZT[dtype])
+        ws = torch.full((max(need, 256),), 255, device=DEV, dtype=torch.uint8)
+        zb.zo_attention_paged(batch, q, q.stride(0), 4, dh ** -0.5, cache, out, 4 * dh, ws, need)
+        assert (_np(out).reshape(copies, 8, -1) == first[None, :, :4 * dh]).all(), (copies, width)
+
+
 def test_far_offsets():
     """Pages beyond 2^31 elements and 2^32 bytes of a pool."""
     P, g, dh = 1024, 8, 128
