@@ -4,12 +4,15 @@
 //   k_embed_rows   X[t] = E[tokens[t]] (+ E_pos[pos[t]]), positions advanced
 //
 // Sampling without a sort.  With the order "logit descending, index ascending" all three filters keep a prefix of a
-// row's tokens, so what has to be found is the prefix's last token, never the order itself.  Weights are
-// w = 2^-d, d = (M - z) log2(e) / T >= 0 in double; a token falls into bin floor(8 d), and a histogram of counts and
-// weights over the bins tells in which bin the prefix ends.  Inside a bin all weights share floor(d), so their
-// mantissas add up as 64-bit integers: the sums are exact and do not depend on the order in which threads add.  The
-// bin where the prefix ends is cut again by the bits of its logits until one value is left, and equal logits are kept by
-// ascending index.  The draw is a prefix sum by index over the kept tokens: sums of 256 tokens, then of one.
+// row's tokens, so what has to be found is the prefix's last token, never the order itself.  Weights are w = 2^-d,
+// d = (M - z) log2(e) / T >= 0 in double; a token falls into bin floor(8 d), and a histogram of counts and weights over the
+// bins tells in which bin the prefix ends.  Sums of weights are sums of 64-bit integers wherever threads add in any order, so
+// they do not depend on it.  The bin where the prefix ends is cut again by the bits of its logits until one value is left,
+// and equal logits are kept by ascending index.  The draw is a search in the kept tokens' running sum by index.
+//
+// One workgroup of 16 waves per row.  A row is read once for its maximum, once for the histogram (counts alone take no
+// exponential: a top-k row needs none for the tokens it drops), and once to gather the tokens that matter into LDS, where
+// the rest happens; only a row that keeps more than kList tokens reads them a third time, for its running sum.
 #include "zo_device.hpp"
 #include "zo_internal.hpp"
 
@@ -18,9 +21,14 @@ namespace {
 
 constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / kWave;
-constexpr int kBins = 1024;          // eighths of d up to 128; the last bin holds the rest (weights below 2^-127: none)
-constexpr int kStrip = 256;          // tokens per partial sum of the draw
-constexpr int kMaxStrips = (1 << 19) / kStrip;
+constexpr int kBins = kThreads;      // eighths of d up to 128; the last bin holds the rest (weights below 2^-127: none)
+constexpr int kLast = kBins - 1;
+constexpr int kStrip = 256;          // tokens that a wave reads at once, four neighbours a lane
+constexpr int kMaxVocab = 1 << 19;
+constexpr int kMaxStrips = kMaxVocab / kStrip;
+constexpr int kList = 4096;          // tokens that fit in LDS
+
+typedef unsigned long long u64;
 
 __device__ __forceinline__ float ld_logit(const float* p, int i) { return p[i]; }
 __device__ __forceinline__ float ld_logit(const bf16_t* p, int i) { return bf16_to_f32(p[i]); }
@@ -32,343 +40,659 @@ __device__ __forceinline__ uint32_t key_of(float z) {
   return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 
-// 2^-f for f in [0, 1): 2^-1/2 times the Taylor polynomial of exp((1/2 - f) ln 2); its first omitted term is below 2e-16.
-__device__ __forceinline__ double exp2_neg(double f) {
-  const double x = (0.5 - f) * 0.6931471805599453094;
-  double p = 1.0 / 479001600.0;
-  p = p * x + 1.0 / 39916800.0;
-  p = p * x + 1.0 / 3628800.0;
-  p = p * x + 1.0 / 362880.0;
-  p = p * x + 1.0 / 40320.0;
-  p = p * x + 1.0 / 5040.0;
-  p = p * x + 1.0 / 720.0;
-  p = p * x + 1.0 / 120.0;
-  p = p * x + 1.0 / 24.0;
-  p = p * x + 1.0 / 6.0;
-  p = p * x + 0.5;
-  p = p * x + 1.0;
-  p = p * x + 1.0;
-  return p * 0.70710678118654752440;
+// Four neighbouring logits from `at`, cleaned; -infinity behind the row's end.
+__device__ __forceinline__ void four(const float* z, int at, int V, bool vec, float (&x)[4]) {
+  if (vec && at + 4 <= V) {
+    const float4 v = *reinterpret_cast<const float4*>(z + at);
+    x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = at + j < V ? z[at + j] : -INFINITY;
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] = clean(x[j]);
+}
+__device__ __forceinline__ void four(const bf16_t* z, int at, int V, bool vec, float (&x)[4]) {
+  if (vec && at + 4 <= V) {
+    const uint2 v = *reinterpret_cast<const uint2*>(z + at);
+    x[0] = __uint_as_float(v.x << 16); x[1] = __uint_as_float(v.x & 0xFFFF0000u);
+    x[2] = __uint_as_float(v.y << 16); x[3] = __uint_as_float(v.y & 0xFFFF0000u);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = at + j < V ? bf16_to_f32(z[at + j]) : -INFINITY;
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] = clean(x[j]);
 }
 
-// How far a logit lies below the row's maximum, and its weight.
+// 2^(-y/8) for y in [0, 1): the Taylor polynomial about 1/2; its first omitted term is below 6e-14 of the value.
+__device__ __forceinline__ double exp2_neg8(double y) {
+  constexpr double kLn = 0.6931471805599453094 / 8, kMid = 0.95760328069857364694;   // ln(2)/8, 2^(-1/16)
+  const double x = 0.5 - y;
+  double p = kMid * kLn * kLn * kLn * kLn * kLn * kLn / 720;
+  p = p * x + kMid * kLn * kLn * kLn * kLn * kLn / 120;
+  p = p * x + kMid * kLn * kLn * kLn * kLn / 24;
+  p = p * x + kMid * kLn * kLn * kLn / 6;
+  p = p * x + kMid * kLn * kLn / 2;
+  p = p * x + kMid * kLn;
+  return p * x + kMid;
+}
+// 2^(-i/8)
+__device__ __forceinline__ double eighth(int i) {
+  const double r[8] = {1.0, 0.91700404320467123174, 0.84089641525371454303, 0.77110541270397041180,
+                       0.70710678118654752440, 0.64841977732550483296, 0.59460355750136053336, 0.54525386633262882960};
+  double x = r[0];
+#pragma unroll
+  for (int j = 1; j < 8; ++j) x = i == j ? r[j] : x;
+  return x;
+}
+
+// How far a logit lies below the row's maximum, in eighths of an octave of its weight.
 struct Scale {
   float zmax;
-  double c;   // log2(e) / T
-  __device__ __forceinline__ double dist(float z) const { return z == zmax ? 0.0 : ((double)zmax - (double)z) * c; }
+  double c8;   // 8 log2(e) / T
+  __device__ __forceinline__ double dist8(float z) const { return z == zmax ? 0.0 : ((double)zmax - (double)z) * c8; }
+  __device__ __forceinline__ int bin(float z) const {
+    const double d = dist8(z);
+    return d < (double)kLast ? (int)d : kLast;
+  }
+  __device__ __forceinline__ double weight(float z) const {
+    const double d = dist8(z);
+    if (!(d < 8000.0)) return 0.0;
+    const int b = (int)d;
+    return ldexp(exp2_neg8(d - b) * eighth(b & 7), -(b >> 3));
+  }
+  // the weight in units of 2^-50 of the maximum's (sums of kList of them fit)
+  __device__ __forceinline__ u64 units(float z) const { return (u64)(weight(z) * 0x1p50 + 0.5); }
 };
-__device__ __forceinline__ int bin_of(double d) { return d < 127.875 ? (int)(d * 8.0) : kBins - 1; }
-// mantissa of a weight as an integer of 2^-44 ulps; the weight is mant * 2^(-44 - floor(d))
-__device__ __forceinline__ uint64_t mant_of(double d) { return (uint64_t)(exp2_neg(d - floor(d)) * 0x1p44 + 0.5); }
-__device__ __forceinline__ double weight_of(double d) { return d < 1000.0 ? ldexp(exp2_neg(d - floor(d)), -(int)d) : 0.0; }
-__device__ __forceinline__ double bin_unit(int bin) { return bin == kBins - 1 ? 0.0 : ldexp(1.0, -44 - (bin >> 3)); }
+// A weight is mant * bin_unit(bin) with mant in units of 2^-44: sums of kMaxVocab mantissas fit into 64 bits.
+__device__ __forceinline__ u64 mant8(double frac) {   // (adding 2^8 leaves units of 2^-44 in the last bits)
+  return (u64)__double_as_longlong(exp2_neg8(frac) + 256.0) - 0x4070000000000000ull;
+}
+__device__ __forceinline__ double bin_unit(int bin) { return bin >= kLast ? 0.0 : ldexp(eighth(bin & 7), -44 - (bin >> 3)); }
 
-__device__ __forceinline__ double wave_sum(double v) {
+template <class T>
+__device__ __forceinline__ T wave_sum(T v) {
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o);
   return v;
 }
-
-// Where the prefix ends: tokens whose logit has a larger key are kept, and of those with this very key the first `ties`.
-struct Cut {
-  uint32_t key;
-  uint32_t ties;
-};
+template <class T>
+__device__ __forceinline__ T wave_scan(T v, int lane) {   // inclusive
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) {
+    const T x = __shfl_up(v, o);
+    if (lane >= o) v += x;
+  }
+  return v;
+}
 
 struct Shared {
   uint32_t cnt[kBins];
-  unsigned long long mass[kBins];
-  double strip[kMaxStrips];
-  float red_z[kWaves];
-  int red_i[kWaves];
-  uint32_t red_n[kWaves];
-  double red_d[kWaves];
+  u64 mass[kBins];
+  union {
+    struct { float z[kList]; int32_t i[kList]; } list;
+    double strip[kMaxStrips];
+  };
+  u64 wave_n[kWaves];
+  double wave_m[kWaves];
+  float wave_z[kWaves];
   // results of one thread, for all
-  uint32_t lo, hi, key, ties, n;
-  int bin;
-  double before, total;
+  uint32_t lo, hi, n_list;
+  int bin, index;
+  u64 n_before, n_at;
+  double m_before, m_at, total;
 };
 
-// What the search for a cut counts: tokens up to `n`, or weight up to `mass` (whichever ends first).
+// What a row's threads share and know.
+template <typename Tio>
+struct Row {
+  Shared& s;
+  const Tio* z;
+  int V, tid, lane, wave;
+  bool vec;
+  Scale sc;
+
+  // f(x, first index) for every four tokens, a strip per wave at a time
+  template <class F>
+  __device__ __forceinline__ void strips(F f) const {
+    const int n = (V + kStrip - 1) / kStrip;
+    for (int st = wave; st < n; st += kWaves) {
+      float x[4];
+      const int at = st * kStrip + lane * 4;
+      four(z, at, V, vec, x);
+      f(x, at);
+    }
+  }
+  // the same with the loads of four strips under way together
+  template <class F>
+  __device__ __forceinline__ void strips4(F f) const {
+    const int n = (V + kStrip - 1) / kStrip;
+    for (int st = wave; st < n; st += 4 * kWaves) {
+      float x[4][4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) four(z, (st + u * kWaves) * kStrip + lane * 4, V, vec, x[u]);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) f(x[u], (st + u * kWaves) * kStrip + lane * 4);
+    }
+  }
+};
+
+// Inclusive running sums over the threads of the workgroup, in a fixed order.  `before` is the sum of the threads before.
+// (Begins and ends with a barrier: the buffers may be in use on either side.)
+__device__ __forceinline__ void block_scan(Shared& s, int lane, int wave, u64 n, double m, u64& n_before, double& m_before) {
+  const u64 ni = wave_scan(n, lane);
+  const double mi = wave_scan(m, lane);
+  __syncthreads();
+  if (lane == kWave - 1) { s.wave_n[wave] = ni; s.wave_m[wave] = mi; }
+  __syncthreads();
+  u64 nb = 0;
+  double mb = 0.0;
+  for (int w = 0; w < wave; ++w) { nb += s.wave_n[w]; mb += s.wave_m[w]; }
+  n_before = nb + ni - n;
+  const double up = __shfl_up(mi, 1);   // (every lane takes part)
+  m_before = lane > 0 ? mb + up : mb;
+  __syncthreads();
+}
+
+// What the search for a cut counts: tokens up to `n`, or weight up to `mass`, whichever ends first.
 struct Goal {
-  uint64_t n;
+  u64 n;
   double mass;
 };
 
-// Finds the first bin at which the running count reaches goal.n or the running weight goal.mass; thread 0's job (the bins
-// are few).  unit(b): weight of one mantissa unit in bin b.
-template <class Unit>
-__device__ int find_bin(const Shared& s, int nbins, const Goal& goal, Unit unit, uint64_t& n, double& mass) {
-  int last = -1;
-  for (int b = 0; b < nbins; ++b) {
-    if (s.cnt[b] == 0) continue;
-    last = b;
-    const double w = (double)s.mass[b] * unit(b);
-    if (n + s.cnt[b] >= goal.n || mass + w >= goal.mass) return b;
-    n += s.cnt[b];
-    mass += w;
+// The first of the workgroup's bins (one a thread: cnt and mass of it) at which the running count reaches goal.n or the running
+// weight goal.mass, the last one in use if a rounding leaves none: s.bin, and what lies before it and in it.
+__device__ __forceinline__ void find_bin(Shared& s, int tid, int lane, int wave, u64 n0, double m0, u64 cnt, double mass,
+                                         const Goal& goal) {
+  u64 nb;
+  double mb;
+  block_scan(s, lane, wave, cnt, mass, nb, mb);
+  nb += n0;
+  mb += m0;
+  const bool used = cnt > 0, hit = used && (nb + cnt >= goal.n || mb + mass >= goal.mass);
+  if (tid == 0) { s.bin = 0x7FFFFFFF; s.index = -1; }
+  __syncthreads();
+  if (hit) atomicMin(&s.bin, tid);
+  if (used) atomicMax(&s.index, tid);
+  __syncthreads();
+  const int at = s.bin != 0x7FFFFFFF ? s.bin : s.index;
+  __syncthreads();
+  if (tid == at) {
+    s.bin = at;
+    s.n_before = nb; s.n_at = cnt;
+    s.m_before = mb; s.m_at = mass;
   }
-  if (last >= 0) {   // (the goal lies beyond the last token by a rounding: the last bin)
-    n -= s.cnt[last];
-    mass -= (double)s.mass[last] * unit(last);
-  }
-  return last;
+  __syncthreads();
 }
 
-// One workgroup per row.
+// Where the prefix ends: tokens whose logit has a larger key are kept, and of those with this very key the ones up to an index.
+struct Cut {
+  uint32_t key;
+  int limit;
+};
+
+// Cuts the tokens of bin `bin` by the bits of their logits.  each(f): f(z, index) for every token of a set that holds the whole
+// bin.  n0, m0: what lies before the bin.  Leaves the key in s.lo, the number of equals to keep in s.n_at, the kept tokens'
+// count in s.n_before + s.n_at and their weight in s.total.
+template <class Each>
+__device__ void refine(Shared& s, const Scale& sc, int tid, int lane, int wave, int bin, u64 n0, double m0, const Goal& goal, Each each) {
+  const double unit = bin_unit(bin);
+  __syncthreads();
+  if (tid == 0) { s.lo = 0xFFFFFFFFu; s.hi = 0; }
+  __syncthreads();
+  uint32_t klo = 0xFFFFFFFFu, khi = 0;
+  each([&](float x, int) {
+    if (sc.bin(x) != bin) return;
+    klo = min(klo, key_of(x));
+    khi = max(khi, key_of(x));
+  });
+  atomicMin(&s.lo, klo);
+  atomicMax(&s.hi, khi);
+  __syncthreads();
+  uint32_t lo = s.lo, hi = s.hi;
+  for (;;) {   // (a round leaves at most a 512th of the keys: four rounds)
+    int shift = 0;
+    while (((hi - lo) >> shift) >= (uint32_t)kBins) ++shift;
+    __syncthreads();
+    s.cnt[tid] = 0;
+    s.mass[tid] = 0;
+    __syncthreads();
+    each([&](float x, int) {
+      const uint32_t key = key_of(x);
+      if (key < lo || key > hi || sc.bin(x) != bin) return;
+      const int b = (int)((hi - key) >> shift);
+      const double d = sc.dist8(x);
+      atomicAdd(&s.cnt[b], 1u);
+      if (bin < kLast) atomicAdd(&s.mass[b], mant8(d - bin));
+    });
+    __syncthreads();
+    find_bin(s, tid, lane, wave, n0, m0, s.cnt[tid], (double)s.mass[tid] * unit, goal);
+    const uint32_t top = hi - ((uint32_t)s.bin << shift);
+    n0 = s.n_before;
+    m0 = s.m_before;
+    if (shift == 0) {
+      if (tid == s.bin) {   // one key: how many of its equals
+        const double w = (double)(s.mass[tid] / s.cnt[tid]) * unit;
+        u64 ties = goal.n > n0 ? goal.n - n0 : 0;
+        if (w > 0.0 && goal.mass < INFINITY) {
+          const double t = ceil((goal.mass - m0) / w);
+          if (t < (double)ties) ties = t > 0.0 ? (u64)t : 0;
+        }
+        if (ties > s.cnt[tid]) ties = s.cnt[tid];
+        if (ties < 1) ties = 1;
+        s.lo = top;
+        s.n_at = ties;
+        s.total = m0 + (double)ties * w;
+      }
+      __syncthreads();
+      return;
+    }
+    const uint32_t width = (1u << shift) - 1;
+    lo = top - lo > width ? top - width : lo;
+    hi = top;
+  }
+}
+
+// The lowest index at which the running sum by index of val(z, index) over a list exceeds `target` (below the whole sum): s.index.
+template <class Val>
+__device__ void list_index(Shared& s, int tid, int lane, int wave, int n, int V, u64 target, Val val) {
+  int shift = 0;
+  while (((V - 1) >> shift) >= kBins) ++shift;   // (at most 9)
+  int first = 0;
+  u64 base = 0;
+#pragma unroll 1
+  for (int level = 0; level < 2; ++level) {   // blocks of indexes, then the indexes of one
+    __syncthreads();
+    s.mass[tid] = 0;
+    __syncthreads();
+    for (int e = tid; e < n; e += kThreads) {
+      const int i = s.list.i[e];
+      const int b = level == 0 ? i >> shift : i - first;
+      if (level == 1 && (b < 0 || b >> shift)) continue;
+      const u64 v = val(s.list.z[e], i);
+      if (v) atomicAdd(&s.mass[b], v);
+    }
+    __syncthreads();
+    u64 nb;
+    double mb;
+    block_scan(s, lane, wave, s.mass[tid], 0.0, nb, mb);
+    if (nb + base <= target && nb + base + s.mass[tid] > target) { s.bin = tid; s.n_before = nb + base; }
+    __syncthreads();
+    first = level == 0 ? s.bin << shift : first + s.bin;
+    base = s.n_before;
+  }
+  if (tid == 0) s.index = first;
+  __syncthreads();
+}
+
 template <typename Tio>
 __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
   Shared& s = *reinterpret_cast<Shared*>(lds);
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int row = blockIdx.x, V = a.V;
-  const Tio* z = (const Tio*)a.z + (int64_t)row * a.ld;
+  Row<Tio> rw{s, (const Tio*)a.z + (int64_t)row * a.ld, V, tid, lane, wave, false, {0.f, 0.0}};
+  rw.vec = ((uintptr_t)rw.z & (4 * sizeof(Tio) - 1)) == 0;
   const float temp = a.temperature[row];
+  const int k = a.top_k ? a.top_k[row] : 0;
+  const float p = a.top_p ? a.top_p[row] : 1.f;
+  const float mp = a.min_p ? a.min_p[row] : 0.f;
   const bool greedy = !(temp > 0.f);
 
-  // ---- maximum, the lowest index that has it, tokens above -infinity
+  // ---- maximum, tokens above -infinity
   float best = -INFINITY;
-  int best_i = 0x7FFFFFFF;
-  uint32_t valid = 0;
-  for (int i = tid; i < V; i += kThreads) {
-    const float x = clean(ld_logit(z, i));
-    if (x > best) { best = x; best_i = i; }
-    valid += x > -INFINITY;
-  }
+  u64 valid = 0;
+  rw.strips4([&](const float (&x)[4], int) {
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) {
-    const float ob = __shfl_xor(best, o);
-    const int oi = __shfl_xor(best_i, o);
-    if (ob > best || (ob == best && oi < best_i)) { best = ob; best_i = oi; }
-    valid += __shfl_xor(valid, o);
-  }
-  if (lane == 0) { s.red_z[wave] = best; s.red_i[wave] = best_i; s.red_n[wave] = valid; }
+    for (int j = 0; j < 4; ++j) {
+      best = fmaxf(best, x[j]);
+      valid += (unsigned)__popcll(__ballot(x[j] > -INFINITY));   // (of the wave)
+    }
+  });
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) best = fmaxf(best, __shfl_xor(best, o));
+  if (lane == 0) { s.wave_z[wave] = best; s.wave_n[wave] = valid; }
+  if (tid == 0) { s.index = 0x7FFFFFFF; s.n_list = 0; }
+  s.cnt[tid] = 0;
+  s.mass[tid] = 0;
   __syncthreads();
-  best = s.red_z[0]; best_i = s.red_i[0]; valid = s.red_n[0];
-  for (int w = 1; w < kWaves; ++w) {
-    if (s.red_z[w] > best || (s.red_z[w] == best && s.red_i[w] < best_i)) { best = s.red_z[w]; best_i = s.red_i[w]; }
-    valid += s.red_n[w];
-  }
+  valid = 0;
+  for (int w = 0; w < kWaves; ++w) { best = fmaxf(best, s.wave_z[w]); valid += s.wave_n[w]; }
   if (valid == 0 || greedy) {
+    if (valid) {   // the lowest index with the maximum
+      int at = 0x7FFFFFFF;
+      rw.strips([&](const float (&x)[4], int i) {
+#pragma unroll
+        for (int j = 3; j >= 0; --j)
+          if (x[j] == best) at = min(at, i + j);
+      });
+      atomicMin(&s.index, at);
+      __syncthreads();
+    }
     if (tid == 0) {
-      a.tokens[row] = valid ? best_i : -1;
+      a.tokens[row] = valid ? s.index : -1;
       if (a.prob) a.prob[row] = valid ? 1.f : 0.f;
       if (a.n_kept) a.n_kept[row] = valid ? 1 : 0;
     }
     return;
   }
-  const Scale sc{best, 1.4426950408889634074 / (double)temp};
-  const int k = a.top_k ? a.top_k[row] : 0;
-  const float p = a.top_p ? a.top_p[row] : 1.f;
-  const float mp = a.min_p ? a.min_p[row] : 0.f;
+  const Scale sc{best, 8.0 * 1.4426950408889634074 / (double)temp};
   const double min_w = mp > 0.f ? (double)mp : 0.0;
+  const bool limit_k = k > 0 && (u64)k < valid, limit_p = p < 1.f;
 
-  // ---- histogram over the bins of d
-  for (int b = tid; b < kBins; b += kThreads) { s.cnt[b] = 0; s.mass[b] = 0; }
-  __syncthreads();
-  for (int i = tid; i < V; i += kThreads) {
-    const float x = clean(ld_logit(z, i));
-    if (!(x > -INFINITY)) continue;
-    const double d = sc.dist(x);
-    const int b = bin_of(d);
-    atomicAdd(&s.cnt[b], 1u);
-    if (b < kBins - 1) atomicAdd(&s.mass[b], (unsigned long long)mant_of(d));
+  // ---- the bins at which the prefix may end.  Tokens of bins [from, to] are gathered; those before `from` are kept.
+  int to = kLast, from = 0, bin_k = kLast;
+  u64 n_k = valid, nb_k = 0;          // tokens that top-k leaves; tokens before its bin
+  double mb_k = 0.0, z_all = 0.0;
+  u64 n_to = valid;                   // tokens of bins [0, to]
+  if (limit_k) {
+    rw.strips4([&](const float (&x)[4], int) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (x[j] > -INFINITY) atomicAdd(&s.cnt[sc.bin(x[j])], 1u);
+    });
+    __syncthreads();
+    find_bin(s, tid, lane, wave, 0, 0.0, s.cnt[tid], 0.0, Goal{(u64)k, INFINITY});
+    bin_k = to = s.bin;
+    nb_k = s.n_before;
+    n_to = s.n_before + s.n_at;
+    n_k = (u64)k;
+    __syncthreads();
   }
-  __syncthreads();
+  // the weights of the bins, where a limit on weight follows and the tokens do not all fit in LDS
+  const bool weigh = limit_p && (!limit_k || n_to > kList);
+  int bin_p = -1;
+  u64 nb_p = 0;
+  double mb_p = 0.0;
+  if (weigh) {
+    __syncthreads();
+    s.cnt[tid] = 0;
+    __syncthreads();
+    rw.strips4([&](const float (&x)[4], int) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (!(x[j] > -INFINITY)) continue;
+        const double d = sc.dist8(x[j]);
+        const int b = d < (double)kLast ? (int)d : kLast;
+        atomicAdd(&s.cnt[b], 1u);
+        if (b < kLast) atomicAdd(&s.mass[b], mant8(d - b));
+      }
+    });
+    __syncthreads();
+    u64 nb;
+    double mb;
+    const u64 cnt = s.cnt[tid];
+    const double mass = (double)s.mass[tid] * bin_unit(tid);
+    block_scan(s, lane, wave, cnt, mass, nb, mb);
+    if (tid == kLast) s.total = mb + mass;
+    if (tid == bin_k) { s.m_before = mb; s.m_at = mass; }
+    __syncthreads();
+    z_all = s.total;
+    mb_k = s.m_before;
+    // Z_k lies between the weight before top-k's bin and the weight with it
+    const double lo = limit_k ? s.m_before : z_all;
+    __syncthreads();
+    find_bin(s, tid, lane, wave, 0, 0.0, cnt, mass, Goal{~0ull, (double)p * lo});
+    bin_p = s.bin;
+    nb_p = s.n_before;
+    mb_p = s.m_before;
+    const u64 with = s.n_before + s.n_at;
+    if (!limit_k) { to = bin_p; n_to = with; }
+    __syncthreads();
+  }
+  if (min_w > 0.0 && !limit_k && !limit_p) {   // (one bin more than the logarithm says: its rounding must not matter)
+    const double d = -log2(min_w) * 8.0;
+    to = d < (double)(kLast - 2) ? (d > 0.0 ? (int)d + 1 : 1) : kLast;
+    n_to = 0;   // (not known: the gathering tells)
+  }
+
+  // ---- the tokens of the prefix in LDS, if they fit
+  const bool cut_needed = limit_k || limit_p;
+  bool whole = (cut_needed || min_w > 0.0) && n_to <= kList;
+  auto gather = [&](int a_bin, int b_bin) {
+    __syncthreads();
+    if (tid == 0) s.n_list = 0;
+    __syncthreads();
+    rw.strips4([&](const float (&x)[4], int at) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (!(x[j] > -INFINITY)) continue;
+        const int b = sc.bin(x[j]);
+        if (b < a_bin || b > b_bin) continue;
+        const uint32_t e = atomicAdd(&s.n_list, 1u);
+        if (e < kList) { s.list.z[e] = x[j]; s.list.i[e] = at + j; }
+      }
+    });
+    __syncthreads();
+  };
+  if (whole) {
+    gather(0, to);
+    whole = s.n_list <= kList;
+  }
+  int n_list = whole ? (int)s.n_list : 0;
+  auto each_listed = [&](auto f) {
+    for (int e = tid; e < n_list; e += kThreads) f(s.list.z[e], s.list.i[e]);
+  };
+  auto each_token = [&](auto f) {
+    rw.strips([&](const float (&x)[4], int at) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (x[j] > -INFINITY) f(x[j], at + j);
+    });
+  };
 
   // ---- the cut: by count, then by weight among what that left
-  Cut cut{0u, 0xFFFFFFFFu};   // keeps everything
-  uint64_t n_cut = valid;
-  double z_k = 0.0;
-  const bool limit_k = k > 0 && (uint32_t)k < valid, limit_p = p < 1.f;
-  for (int pass = 0; pass < 2; ++pass) {
-    if (pass == 0 ? !limit_k : !limit_p) {
-      if (pass == 0 && limit_p) {   // Z_k is the weight of all tokens
-        if (tid == 0) {
-          double m = 0.0;
-          for (int b = 0; b < kBins; ++b) m += (double)s.mass[b] * bin_unit(b);
-          s.total = m;
-        }
-        __syncthreads();
-        z_k = s.total;
-        __syncthreads();
-      }
-      continue;
-    }
-    const Goal goal = pass == 0 ? Goal{(uint64_t)k, INFINITY} : Goal{n_cut, (double)p * z_k};
-    // bins of d
-    if (tid == 0) {
-      uint64_t n = 0;
-      double m = 0.0;
-      s.bin = find_bin(s, kBins, goal, bin_unit, n, m);
-      s.n = (uint32_t)n;
-      s.before = m;
-      s.lo = 0xFFFFFFFFu;
-      s.hi = 0;
-    }
-    __syncthreads();
-    const int bin = s.bin;
-    const double unit = bin_unit(bin);
-    // the range of its keys
-    uint32_t klo = 0xFFFFFFFFu, khi = 0;
-    for (int i = tid; i < V; i += kThreads) {
-      const float x = clean(ld_logit(z, i));
-      if (!(x > -INFINITY) || bin_of(sc.dist(x)) != bin) continue;
-      klo = min(klo, key_of(x));
-      khi = max(khi, key_of(x));
-    }
-    atomicMin(&s.lo, klo);
-    atomicMax(&s.hi, khi);
-    __syncthreads();
-    uint32_t lo = s.lo, hi = s.hi;
-    // cut by the keys, from the largest down, until one is left
-    __shared__ uint32_t sub_cnt[kBins];
-    __shared__ unsigned long long sub_mass[kBins];
-    for (;;) {
-      int shift = 0;
-      while (((hi - lo) >> shift) >= (uint32_t)kBins) ++shift;
+  Cut cut{0u, 0x7FFFFFFF};   // keeps everything
+  u64 ties = 0;
+  if (limit_k) {
+    const Goal goal{n_k, INFINITY};
+    if (whole && !weigh) {
+      // (the weights before the bin are those of the list)
+      u64 u = 0;
+      each_listed([&](float x, int) { u += sc.bin(x) < bin_k ? sc.units(x) : 0; });
+      u64 nb;
+      double mb;
+      block_scan(s, lane, wave, u, 0.0, nb, mb);
+      if (tid == kThreads - 1) s.m_before = (double)(nb + u) * 0x1p-50;
       __syncthreads();
-      for (int b = tid; b < kBins; b += kThreads) { sub_cnt[b] = 0; sub_mass[b] = 0; }
+      mb_k = s.m_before;
       __syncthreads();
-      for (int i = tid; i < V; i += kThreads) {
-        const float x = clean(ld_logit(z, i));
-        if (!(x > -INFINITY)) continue;
-        const uint32_t key = key_of(x);
-        if (key < lo || key > hi) continue;
-        const double d = sc.dist(x);
-        atomicAdd(&sub_cnt[(hi - key) >> shift], 1u);
-        if (bin < kBins - 1) atomicAdd(&sub_mass[(hi - key) >> shift], (unsigned long long)mant_of(d));
-      }
-      __syncthreads();
-      if (tid == 0) {
-        uint64_t n = s.n;
-        double m = s.before;
-        int last = -1;
-        uint64_t n_last = n;
-        double m_last = m;
-        for (int b = 0; b < kBins; ++b) {
-          if (sub_cnt[b] == 0) continue;
-          last = b; n_last = n; m_last = m;
-          const double w = (double)sub_mass[b] * unit;
-          if (n + sub_cnt[b] >= goal.n || m + w >= goal.mass) break;
-          n += sub_cnt[b];
-          m += w;
-        }
-        s.bin = last;
-        s.n = (uint32_t)n_last;
-        s.before = m_last;
-        if (last >= 0 && shift == 0) {   // one key: how many of its equals
-          const double w = (double)(sub_mass[last] / sub_cnt[last]) * unit;
-          uint64_t ties = goal.n > n_last ? goal.n - n_last : 0;
-          if (w > 0.0 && goal.mass < INFINITY) {
-            const double t = ceil((goal.mass - m_last) / w);
-            if (t < (double)ties) ties = t > 0.0 ? (uint64_t)t : 0;
-          }
-          if (ties > sub_cnt[last]) ties = sub_cnt[last];
-          if (ties < 1) ties = 1;
-          s.ties = (uint32_t)ties;
-          s.total = m_last + (double)ties * w;
-        }
-      }
-      __syncthreads();
-      const uint32_t top = hi - ((uint32_t)s.bin << shift);
-      hi = top;
-      if (shift == 0) { cut.key = top; cut.ties = s.ties; break; }
-      const uint32_t width = (1u << shift) - 1;
-      lo = top - lo > width ? top - width : lo;
     }
-    n_cut = (uint64_t)s.n + s.ties;
-    z_k = s.total;
+    if (whole) refine(s, sc, tid, lane, wave, bin_k, nb_k, mb_k, goal, each_listed);
+    else refine(s, sc, tid, lane, wave, bin_k, nb_k, mb_k, goal, each_token);
+    cut.key = s.lo;
+    ties = s.n_at;
+    z_all = s.total;
     __syncthreads();
   }
-
-  // ---- the draw.  Equal logits at the cut are kept by ascending index: limit = index of the last one
-  int limit = 0x7FFFFFFF;
-  if (cut.ties != 0xFFFFFFFFu) {
-    uint32_t seen = 0;
-    for (int base = 0; base < V; base += kThreads) {
-      const int i = base + tid;
-      const bool hit = i < V && key_of(clean(ld_logit(z, i))) == cut.key;
-      const unsigned long long mask = __ballot(hit);
-      if (lane == 0) s.red_n[wave] = __popcll(mask);
+  if (limit_p) {
+    const Goal goal{n_k, (double)p * z_all};
+    // the bin: among those of the list, or of the histogram (its counts and weights have been overwritten if top-k came before)
+    if (limit_k) {
+      s.cnt[tid] = 0;
+      s.mass[tid] = 0;
       __syncthreads();
-      uint32_t off = seen, all = seen;
-      for (int w = 0; w < kWaves; ++w) { if (w < wave) off += s.red_n[w]; all += s.red_n[w]; }
-      if (hit && off + __popcll(mask & ((1ull << lane) - 1)) == cut.ties - 1) s.key = (uint32_t)i;
+      auto add = [&](float x, int) {
+        const double d = sc.dist8(x);
+        const int b = d < (double)kLast ? (int)d : kLast;
+        if (b > bin_k) return;
+        atomicAdd(&s.cnt[b], 1u);
+        if (b < kLast) atomicAdd(&s.mass[b], mant8(d - b));
+      };
+      if (whole) each_listed(add);
+      else each_token(add);
       __syncthreads();
-      seen = all;
-      if (seen >= cut.ties) break;
+      find_bin(s, tid, lane, wave, 0, 0.0, s.cnt[tid], (double)s.mass[tid] * bin_unit(tid), goal);
+      bin_p = s.bin;
+      nb_p = s.n_before;
+      mb_p = s.m_before;
+      __syncthreads();
     }
-    limit = (int)s.key;
+    if (whole) {
+      refine(s, sc, tid, lane, wave, bin_p, nb_p, mb_p, goal, each_listed);
+    } else {
+      gather(bin_p, bin_p);
+      if (s.n_list <= kList) {
+        n_list = (int)s.n_list;
+        refine(s, sc, tid, lane, wave, bin_p, nb_p, mb_p, goal, each_listed);
+      } else {
+        refine(s, sc, tid, lane, wave, bin_p, nb_p, mb_p, goal, each_token);
+      }
+    }
+    cut.key = s.lo;
+    ties = s.n_at;
+    __syncthreads();
   }
-  auto weight = [&](int i) -> double {   // of token i; negative: not kept
-    const float x = clean(ld_logit(z, i));
+  // ---- equal logits at the cut are kept by ascending index
+  if (cut_needed) {
+    if (whole) {
+      list_index(s, tid, lane, wave, n_list, V, ties - 1, [&](float x, int) { return (u64)(key_of(x) == cut.key); });
+      cut.limit = s.index;
+      __syncthreads();
+    } else {
+      // strips of all waves at a time, in order
+      u64 seen = 0;
+      const int n = (V + kStrip - 1) / kStrip;
+      for (int st = 0; st < n; st += kWaves) {
+        float x[4];
+        const int at = (st + wave) * kStrip + lane * 4;
+        four(rw.z, at, V, rw.vec, x);
+        u64 mine = 0, nb;
+        double mb;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) mine += x[j] > -INFINITY && key_of(x[j]) == cut.key;
+        block_scan(s, lane, wave, mine, 0.0, nb, mb);
+        nb += seen;
+        if (nb < ties && nb + mine >= ties) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (x[j] > -INFINITY && key_of(x[j]) == cut.key && ++nb == ties) s.index = at + j;
+        }
+        if (tid == kThreads - 1) s.n_at = nb < ties || mine == 0 ? nb + mine : ties;
+        __syncthreads();
+        seen = s.n_at;
+        __syncthreads();
+        if (seen >= ties) break;
+      }
+      cut.limit = s.index;
+      __syncthreads();
+    }
+  }
+  auto kept = [&](float x, int i) {   // (of a token above -infinity)
     const uint32_t key = key_of(x);
-    if (!(x > -INFINITY) || key < cut.key || (key == cut.key && i > limit)) return -1.0;
-    const double w = weight_of(sc.dist(x));
-    return (w >= min_w || x == sc.zmax) ? w : -1.0;
+    return key > cut.key || (key == cut.key && i <= cut.limit);
+  };
+  const float u0 = a.u[row];
+  const double u1 = u0 > 0.f ? (u0 < 1.f ? (double)u0 : 1.0) : 0.0;
+
+  // ---- the draw
+  if (whole) {
+    auto val = [&](float x, int i) -> u64 {
+      if (!kept(x, i)) return 0;
+      const double w = sc.weight(x);
+      return w >= min_w || x == sc.zmax ? (u64)(w * 0x1p50 + 0.5) : 0;
+    };
+    u64 sum = 0, number = 0;
+    each_listed([&](float x, int i) {
+      if (!kept(x, i)) return;
+      const double w = sc.weight(x);
+      if (!(w >= min_w || x == sc.zmax)) return;
+      ++number;
+      sum += (u64)(w * 0x1p50 + 0.5);
+    });
+    sum = wave_sum(sum);
+    number = wave_sum(number);
+    __syncthreads();
+    if (lane == 0) { s.wave_n[wave] = sum; s.mass[wave] = number; }
+    __syncthreads();
+    sum = number = 0;
+    for (int w = 0; w < kWaves; ++w) { sum += s.wave_n[w]; number += s.mass[w]; }
+    u64 target = (u64)(u1 * (double)sum);
+    if (target >= sum) target = sum - 1;   // (the last token with a weight)
+    list_index(s, tid, lane, wave, n_list, V, target, val);
+    if (tid == 0) {
+      const int i = s.index;
+      a.tokens[row] = i;
+      if (a.prob) a.prob[row] = (float)(sc.weight(clean(ld_logit(rw.z, i))) / ((double)sum * 0x1p-50));
+      if (a.n_kept) a.n_kept[row] = (int32_t)number;
+    }
+    return;
+  }
+  auto weight = [&](float x, int i) -> double {   // negative: not kept
+    if (!(x > -INFINITY) || !kept(x, i)) return -1.0;
+    const double w = sc.weight(x);
+    return w >= min_w || x == sc.zmax ? w : -1.0;
   };
   const int strips = (V + kStrip - 1) / kStrip;
-  uint32_t kept = 0;
-  for (int st = wave; st < strips; st += kWaves) {
+  u64 number = 0;
+  __syncthreads();   // (the strips' sums take the list's place)
+  rw.strips4([&](const float (&x)[4], int at) {
     double sum = 0.0;
 #pragma unroll
-    for (int j = 0; j < kStrip / kWave; ++j) {
-      const int i = st * kStrip + j * kWave + lane;
-      const double w = i < V ? weight(i) : -1.0;
-      if (w >= 0.0) { sum += w; ++kept; }
+    for (int j = 0; j < 4; ++j) {
+      const double w = weight(x[j], at + j);
+      number += (unsigned)__popcll(__ballot(w >= 0.0));
+      sum += w > 0.0 ? w : 0.0;
     }
     sum = wave_sum(sum);
-    if (lane == 0) s.strip[st] = sum;
-  }
+    if (lane == 0 && at < V) s.strip[at / kStrip] = sum;
+  });
+  if (lane == 0) s.wave_n[wave] = number;
+  __syncthreads();
+  number = 0;
+  for (int w = 0; w < kWaves; ++w) number += s.wave_n[w];
+  // a thread has two neighbouring strips: their running sum passes the target in one of them
+  double sum[2], mb;
+  u64 nb;
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) kept += __shfl_xor(kept, o);
-  if (lane == 0) s.red_n[wave] = kept;
+  for (int j = 0; j < 2; ++j) sum[j] = tid * 2 + j < strips ? s.strip[tid * 2 + j] : 0.0;
+  block_scan(s, lane, wave, 0, sum[0] + sum[1], nb, mb);
+  if (tid == kThreads - 1) s.total = mb + (sum[0] + sum[1]);
+  if (tid == 0) { s.bin = 0x7FFFFFFF; s.index = -1; }
+  __syncthreads();
+  const double total = s.total, target = u1 * total;
+  int hit = -1;
+#pragma unroll
+  for (int j = 1; j >= 0; --j) {
+    const double inc = j ? mb + (sum[0] + sum[1]) : mb + sum[0];
+    if (sum[j] > 0.0 && inc > target) hit = tid * 2 + j;
+  }
+  if (hit >= 0) atomicMin(&s.bin, hit);
+  if (sum[0] > 0.0 || sum[1] > 0.0) atomicMax(&s.index, tid * 2 + (sum[1] > 0.0));
+  __syncthreads();
+  const int at = s.bin != 0x7FFFFFFF ? s.bin : s.index;   // (the last strip with a weight if rounding leaves none)
+  if (tid == at / 2) s.m_before = at & 1 ? mb + sum[0] : mb;
   __syncthreads();
   if (wave != 0) return;
-  kept = 0;
-  for (int w = 0; w < kWaves; ++w) kept += s.red_n[w];
-  double total = 0.0;
-  for (int st = 0; st < strips; ++st) total += s.strip[st];
-  const float u0 = a.u[row];
-  const double target = (u0 > 0.f ? (u0 < 1.f ? (double)u0 : 1.0) : 0.0) * total;
-  // the strip in which the running sum passes the target; the last one with a weight if rounding leaves none
-  int at = 0;
-  double before = 0.0, run = 0.0;
-  for (int st = 0; st < strips; ++st) {
-    if (!(s.strip[st] > 0.0)) continue;
-    at = st;
-    before = run;
-    run += s.strip[st];
-    if (run > target) break;
-  }
-  // and the token in the strip
-  int token = -1;
-  double w_token = 0.0;
-  for (int j = 0; j < kStrip / kWave; ++j) {
-    const int i = at * kStrip + j * kWave + lane;
-    const double w0 = i < V ? weight(i) : -1.0;
-    const double w = w0 > 0.0 ? w0 : 0.0;
-    double inc = w;
+  // and the token in the strip: four neighbours a lane
+  float x[4];
+  double w[4], run = 0.0;
+  four(rw.z, at * kStrip + lane * 4, V, rw.vec, x);
 #pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-      const double v = __shfl_up(inc, o);
-      if (lane >= o) inc += v;
-    }
-    const unsigned long long has = __ballot(w > 0.0);
-    const unsigned long long pass = __ballot(w > 0.0 && before + inc > target);
-    if (has) {
-      const int src = pass ? __ffsll((long long)pass) - 1 : 63 - __clzll((long long)has);
-      token = at * kStrip + j * kWave + src;
-      w_token = __shfl(w, src);
-      if (pass) break;
-    }
-    before += __shfl(inc, kWave - 1);
+  for (int j = 0; j < 4; ++j) {
+    w[j] = weight(x[j], at * kStrip + lane * 4 + j);
+    if (!(w[j] > 0.0)) w[j] = 0.0;
+    run += w[j];
   }
-  if (lane == 0) {
-    a.tokens[row] = token;
-    if (a.prob) a.prob[row] = (float)(w_token / total);
-    if (a.n_kept) a.n_kept[row] = (int32_t)kept;
+  double before = s.m_before + (wave_scan(run, lane) - run);
+  int mine = -1, last = -1;
+  double w_mine = 0.0, w_last = 0.0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    before += w[j];
+    if (w[j] > 0.0) {
+      if (mine < 0 && before > target) { mine = j; w_mine = w[j]; }
+      last = j;
+      w_last = w[j];
+    }
+  }
+  const u64 pass = __ballot(mine >= 0), has = __ballot(last >= 0);
+  const int src = pass ? __ffsll((long long)pass) - 1 : 63 - __clzll((long long)has);
+  if (lane == src) {
+    a.tokens[row] = at * kStrip + lane * 4 + (pass ? mine : last);
+    if (a.prob) a.prob[row] = (float)((pass ? w_mine : w_last) / total);
+    if (a.n_kept) a.n_kept[row] = (int32_t)number;
   }
 }
 
