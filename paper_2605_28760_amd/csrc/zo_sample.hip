@@ -23,7 +23,8 @@ constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kBins = kThreads;      // eighths of d up to 128; the last bin holds the rest (weights below 2^-127: none)
 constexpr int kLast = kBins - 1;
-constexpr int kStrip = 256;          // tokens that a wave reads at once, four neighbours a lane
+constexpr int kPieces = 4;           // loads of a wave under way, four neighbouring tokens a lane each
+constexpr int kStrip = kPieces * 4 * kWave;
 constexpr int kMaxVocab = 1 << 19;
 constexpr int kMaxStrips = kMaxVocab / kStrip;
 constexpr int kList = 4096;          // tokens that fit in LDS
@@ -40,42 +41,36 @@ __device__ __forceinline__ uint32_t key_of(float z) {
   return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 
-// Four neighbouring logits from `at`, cleaned; -infinity behind the row's end.
-__device__ __forceinline__ void four(const float* z, int at, int V, bool vec, float (&x)[4]) {
-  if (vec && at + 4 <= V) {
-    const float4 v = *reinterpret_cast<const float4*>(z + at);
-    x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
-  } else {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = at + j < V ? z[at + j] : -INFINITY;
-  }
-#pragma unroll
-  for (int j = 0; j < 4; ++j) x[j] = clean(x[j]);
+// Four neighbouring logits as they lie in memory.
+template <typename Tio> struct Raw;
+template <> struct Raw<float> { typedef float4 type; };
+template <> struct Raw<bf16_t> { typedef uint2 type; };
+__device__ __forceinline__ void unpack(const float4& v, float (&x)[4]) {
+  x[0] = clean(v.x); x[1] = clean(v.y); x[2] = clean(v.z); x[3] = clean(v.w);
 }
-__device__ __forceinline__ void four(const bf16_t* z, int at, int V, bool vec, float (&x)[4]) {
-  if (vec && at + 4 <= V) {
-    const uint2 v = *reinterpret_cast<const uint2*>(z + at);
-    x[0] = __uint_as_float(v.x << 16); x[1] = __uint_as_float(v.x & 0xFFFF0000u);
-    x[2] = __uint_as_float(v.y << 16); x[3] = __uint_as_float(v.y & 0xFFFF0000u);
-  } else {
+__device__ __forceinline__ void unpack(const uint2& v, float (&x)[4]) {
+  x[0] = clean(__uint_as_float(v.x << 16)); x[1] = clean(__uint_as_float(v.x & 0xFFFF0000u));
+  x[2] = clean(__uint_as_float(v.y << 16)); x[3] = clean(__uint_as_float(v.y & 0xFFFF0000u));
+}
+// Four from `at` of a row of any alignment and end: -infinity behind it.
+template <typename Tio>
+__device__ __forceinline__ void four(const Tio* z, int at, int V, float (&x)[4]) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = at + j < V ? bf16_to_f32(z[at + j]) : -INFINITY;
-  }
-#pragma unroll
-  for (int j = 0; j < 4; ++j) x[j] = clean(x[j]);
+  for (int j = 0; j < 4; ++j) x[j] = at + j < V ? clean(ld_logit(z, at + j)) : -INFINITY;
 }
 
-// 2^(-y/8) for y in [0, 1): the Taylor polynomial about 1/2; its first omitted term is below 6e-14 of the value.
+// 2^(-y/8) for y in [0, 1): the Taylor polynomial about 0; its first omitted term is below 8e-14.  Exactly 1 at 0: rows of equal
+// logits have weights whose sums are exact, and so have u * Z between two of them.
 __device__ __forceinline__ double exp2_neg8(double y) {
-  constexpr double kLn = 0.6931471805599453094 / 8, kMid = 0.95760328069857364694;   // ln(2)/8, 2^(-1/16)
-  const double x = 0.5 - y;
-  double p = kMid * kLn * kLn * kLn * kLn * kLn * kLn / 720;
-  p = p * x + kMid * kLn * kLn * kLn * kLn * kLn / 120;
-  p = p * x + kMid * kLn * kLn * kLn * kLn / 24;
-  p = p * x + kMid * kLn * kLn * kLn / 6;
-  p = p * x + kMid * kLn * kLn / 2;
-  p = p * x + kMid * kLn;
-  return p * x + kMid;
+  constexpr double kLn = -0.6931471805599453094 / 8;
+  double p = kLn * kLn * kLn * kLn * kLn * kLn * kLn / 5040;
+  p = p * y + kLn * kLn * kLn * kLn * kLn * kLn / 720;
+  p = p * y + kLn * kLn * kLn * kLn * kLn / 120;
+  p = p * y + kLn * kLn * kLn * kLn / 24;
+  p = p * y + kLn * kLn * kLn / 6;
+  p = p * y + kLn * kLn / 2;
+  p = p * y + kLn;
+  return p * y + 1.0;
 }
 // 2^(-i/8)
 __device__ __forceinline__ double eighth(int i) {
@@ -153,28 +148,38 @@ struct Row {
   bool vec;
   Scale sc;
 
-  // f(x, first index) for every four tokens, a strip per wave at a time
-  template <class F>
-  __device__ __forceinline__ void strips(F f) const {
-    const int n = (V + kStrip - 1) / kStrip;
-    for (int st = wave; st < n; st += kWaves) {
-      float x[4];
-      const int at = st * kStrip + lane * 4;
-      four(z, at, V, vec, x);
-      f(x, at);
+  // f(x, first index) for every four tokens of a strip of kStrip tokens, strip by strip of this wave's share, then
+  // done(strip).  A whole strip's loads are under way together; they are not conditional, or the next would wait for the last.
+  template <class F, class Done>
+  __device__ __forceinline__ void strips(F f, Done done) const {
+    const int n = (V + kStrip - 1) / kStrip, whole = vec ? V / kStrip : 0;
+    typedef typename Raw<Tio>::type R;
+    int st = wave;
+    for (; st < whole; st += kWaves) {
+      R raw[kPieces];
+#pragma unroll
+      for (int u = 0; u < kPieces; ++u) raw[u] = *reinterpret_cast<const R*>(z + st * kStrip + u * (4 * kWave) + lane * 4);
+#pragma unroll
+      for (int u = 0; u < kPieces; ++u) {
+        float x[4];
+        unpack(raw[u], x);
+        f(x, st * kStrip + u * (4 * kWave) + lane * 4);
+      }
+      done(st);
+    }
+    for (; st < n; st += kWaves) {
+      for (int u = 0; u < kPieces; ++u) {
+        float x[4];
+        const int at = st * kStrip + u * (4 * kWave) + lane * 4;
+        four(z, at, V, x);
+        f(x, at);
+      }
+      done(st);
     }
   }
-  // the same with the loads of four strips under way together
   template <class F>
-  __device__ __forceinline__ void strips4(F f) const {
-    const int n = (V + kStrip - 1) / kStrip;
-    for (int st = wave; st < n; st += 4 * kWaves) {
-      float x[4][4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) four(z, (st + u * kWaves) * kStrip + lane * 4, V, vec, x[u]);
-#pragma unroll
-      for (int u = 0; u < 4; ++u) f(x[u], (st + u * kWaves) * kStrip + lane * 4);
-    }
+  __device__ __forceinline__ void strips(F f) const {
+    strips(f, [](int) {});
   }
 };
 
@@ -333,7 +338,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int row = blockIdx.x, V = a.V;
   Row<Tio> rw{s, (const Tio*)a.z + (int64_t)row * a.ld, V, tid, lane, wave, false, {0.f, 0.0}};
-  rw.vec = ((uintptr_t)rw.z & (4 * sizeof(Tio) - 1)) == 0;
+  rw.vec = ((uintptr_t)rw.z & (4 * sizeof(Tio) - 1)) == 0;   // (a row whose four tokens do not start on their size goes one by one)
   const float temp = a.temperature[row];
   const int k = a.top_k ? a.top_k[row] : 0;
   const float p = a.top_p ? a.top_p[row] : 1.f;
@@ -343,7 +348,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
   // ---- maximum, tokens above -infinity
   float best = -INFINITY;
   u64 valid = 0;
-  rw.strips4([&](const float (&x)[4], int) {
+  rw.strips([&](const float (&x)[4], int) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       best = fmaxf(best, x[j]);
@@ -387,7 +392,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
   double mb_k = 0.0, z_all = 0.0;
   u64 n_to = valid;                   // tokens of bins [0, to]
   if (limit_k) {
-    rw.strips4([&](const float (&x)[4], int) {
+    rw.strips([&](const float (&x)[4], int) {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         if (x[j] > -INFINITY) atomicAdd(&s.cnt[sc.bin(x[j])], 1u);
@@ -409,7 +414,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
     __syncthreads();
     s.cnt[tid] = 0;
     __syncthreads();
-    rw.strips4([&](const float (&x)[4], int) {
+    rw.strips([&](const float (&x)[4], int) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         if (!(x[j] > -INFINITY)) continue;
@@ -454,7 +459,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
     __syncthreads();
     if (tid == 0) s.n_list = 0;
     __syncthreads();
-    rw.strips4([&](const float (&x)[4], int at) {
+    rw.strips([&](const float (&x)[4], int at) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         if (!(x[j] > -INFINITY)) continue;
@@ -551,13 +556,12 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
       cut.limit = s.index;
       __syncthreads();
     } else {
-      // strips of all waves at a time, in order
+      // four tokens of every thread at a time, in order
       u64 seen = 0;
-      const int n = (V + kStrip - 1) / kStrip;
-      for (int st = 0; st < n; st += kWaves) {
+      for (int first = 0; first < V; first += 4 * kThreads) {
         float x[4];
-        const int at = (st + wave) * kStrip + lane * 4;
-        four(rw.z, at, V, rw.vec, x);
+        const int at = first + tid * 4;
+        four(rw.z, at, V, x);
         u64 mine = 0, nb;
         double mb;
 #pragma unroll
@@ -626,72 +630,86 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
   };
   const int strips = (V + kStrip - 1) / kStrip;
   u64 number = 0;
+  double part = 0.0;
   __syncthreads();   // (the strips' sums take the list's place)
-  rw.strips4([&](const float (&x)[4], int at) {
-    double sum = 0.0;
+  rw.strips(
+      [&](const float (&x)[4], int at) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const double w = weight(x[j], at + j);
-      number += (unsigned)__popcll(__ballot(w >= 0.0));
-      sum += w > 0.0 ? w : 0.0;
-    }
-    sum = wave_sum(sum);
-    if (lane == 0 && at < V) s.strip[at / kStrip] = sum;
-  });
+        for (int j = 0; j < 4; ++j) {
+          const double w = weight(x[j], at + j);
+          number += (unsigned)__popcll(__ballot(w >= 0.0));
+          part += w > 0.0 ? w : 0.0;
+        }
+      },
+      [&](int st) {
+        const double sum = wave_sum(part);
+        if (lane == 0) s.strip[st] = sum;
+        part = 0.0;
+      });
   if (lane == 0) s.wave_n[wave] = number;
   __syncthreads();
   number = 0;
   for (int w = 0; w < kWaves; ++w) number += s.wave_n[w];
-  // a thread has two neighbouring strips: their running sum passes the target in one of them
-  double sum[2], mb;
+  // a strip a thread: the running sum passes the target in one of them
+  const double sum = tid < strips ? s.strip[tid] : 0.0;
+  double mb;
   u64 nb;
-#pragma unroll
-  for (int j = 0; j < 2; ++j) sum[j] = tid * 2 + j < strips ? s.strip[tid * 2 + j] : 0.0;
-  block_scan(s, lane, wave, 0, sum[0] + sum[1], nb, mb);
-  if (tid == kThreads - 1) s.total = mb + (sum[0] + sum[1]);
+  block_scan(s, lane, wave, 0, sum, nb, mb);
+  if (tid == kThreads - 1) s.total = mb + sum;
   if (tid == 0) { s.bin = 0x7FFFFFFF; s.index = -1; }
   __syncthreads();
   const double total = s.total, target = u1 * total;
-  int hit = -1;
-#pragma unroll
-  for (int j = 1; j >= 0; --j) {
-    const double inc = j ? mb + (sum[0] + sum[1]) : mb + sum[0];
-    if (sum[j] > 0.0 && inc > target) hit = tid * 2 + j;
+  if (sum > 0.0) {
+    if (mb + sum > target) atomicMin(&s.bin, tid);
+    atomicMax(&s.index, tid);
   }
-  if (hit >= 0) atomicMin(&s.bin, hit);
-  if (sum[0] > 0.0 || sum[1] > 0.0) atomicMax(&s.index, tid * 2 + (sum[1] > 0.0));
   __syncthreads();
-  const int at = s.bin != 0x7FFFFFFF ? s.bin : s.index;   // (the last strip with a weight if rounding leaves none)
-  if (tid == at / 2) s.m_before = at & 1 ? mb + sum[0] : mb;
+  const bool passed = s.bin != 0x7FFFFFFF;
+  const int at = passed ? s.bin : s.index;   // (the last strip with a weight if rounding leaves none)
+  if (tid == at) s.m_before = mb;
   __syncthreads();
   if (wave != 0) return;
-  // and the token in the strip: four neighbours a lane
-  float x[4];
-  double w[4], run = 0.0;
-  four(rw.z, at * kStrip + lane * 4, V, rw.vec, x);
+  // and the token in the strip
+  double before = s.m_before, w_token = 0.0;
+  int token = -1;
+  for (int u = 0; u < kPieces; ++u) {
+    float x[4];
+    double w[4], run = 0.0;
+    const int first = at * kStrip + u * (4 * kWave) + lane * 4;
+    four(rw.z, first, V, x);
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    w[j] = weight(x[j], at * kStrip + lane * 4 + j);
-    if (!(w[j] > 0.0)) w[j] = 0.0;
-    run += w[j];
-  }
-  double before = s.m_before + (wave_scan(run, lane) - run);
-  int mine = -1, last = -1;
-  double w_mine = 0.0, w_last = 0.0;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    before += w[j];
-    if (w[j] > 0.0) {
-      if (mine < 0 && before > target) { mine = j; w_mine = w[j]; }
-      last = j;
-      w_last = w[j];
+    for (int j = 0; j < 4; ++j) {
+      w[j] = weight(x[j], first + j);
+      if (!(w[j] > 0.0)) w[j] = 0.0;
+      run += w[j];
     }
+    const double inc = wave_scan(run, lane);
+    double b = before + (inc - run);
+    int mine = -1, last = -1;
+    double w_mine = 0.0, w_last = 0.0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      b += w[j];
+      if (w[j] > 0.0) {
+        if (mine < 0 && b > target) { mine = first + j; w_mine = w[j]; }
+        last = first + j;
+        w_last = w[j];
+      }
+    }
+    const u64 pass = __ballot(mine >= 0), has = __ballot(last >= 0);
+    if (has) {
+      const int src = pass ? __ffsll((long long)pass) - 1 : 63 - __clzll((long long)has);
+      const int i = pass ? mine : last;
+      const double wi = pass ? w_mine : w_last;
+      token = __shfl(i, src);
+      w_token = __shfl(wi, src);
+      if (pass) break;
+    }
+    before += __shfl(inc, kWave - 1);
   }
-  const u64 pass = __ballot(mine >= 0), has = __ballot(last >= 0);
-  const int src = pass ? __ffsll((long long)pass) - 1 : 63 - __clzll((long long)has);
-  if (lane == src) {
-    a.tokens[row] = at * kStrip + lane * 4 + (pass ? mine : last);
-    if (a.prob) a.prob[row] = (float)((pass ? w_mine : w_last) / total);
+  if (lane == 0) {
+    a.tokens[row] = token;
+    if (a.prob) a.prob[row] = (float)(w_token / total);
     if (a.n_kept) a.n_kept[row] = (int32_t)number;
   }
 }
