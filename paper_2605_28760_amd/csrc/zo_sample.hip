@@ -33,34 +33,36 @@ typedef unsigned long long u64;
 
 __device__ __forceinline__ float ld_logit(const float* p, int i) { return p[i]; }
 __device__ __forceinline__ float ld_logit(const bf16_t* p, int i) { return bf16_to_f32(p[i]); }
-// NaN counts as -infinity, -0 as 0
-__device__ __forceinline__ float clean(float z) { return z != z ? -INFINITY : z + 0.0f; }
-// Unsigned integers in the order of the floats.
+// Neither NaN nor -infinity.  (Compared with the least number, not with -infinity: "above -infinity" is compiled into a
+// comparison that NaN passes.)
+constexpr float kLeast = -3.402823466e38f;
+__device__ __forceinline__ bool is_token(float z) { return z >= kLeast; }
+// Unsigned integers in the order of the floats, and back; -0 is 0.
 __device__ __forceinline__ uint32_t key_of(float z) {
-  const uint32_t u = __float_as_uint(z);
+  const uint32_t u = __float_as_uint(z + 0.0f);
   return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
+__device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
 
 // Four neighbouring logits as they lie in memory.
 template <typename Tio> struct Raw;
 template <> struct Raw<float> { typedef float4 type; };
 template <> struct Raw<bf16_t> { typedef uint2 type; };
 __device__ __forceinline__ void unpack(const float4& v, float (&x)[4]) {
-  x[0] = clean(v.x); x[1] = clean(v.y); x[2] = clean(v.z); x[3] = clean(v.w);
+  x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
 }
 __device__ __forceinline__ void unpack(const uint2& v, float (&x)[4]) {
-  x[0] = clean(__uint_as_float(v.x << 16)); x[1] = clean(__uint_as_float(v.x & 0xFFFF0000u));
-  x[2] = clean(__uint_as_float(v.y << 16)); x[3] = clean(__uint_as_float(v.y & 0xFFFF0000u));
+  x[0] = __uint_as_float(v.x << 16); x[1] = __uint_as_float(v.x & 0xFFFF0000u);
+  x[2] = __uint_as_float(v.y << 16); x[3] = __uint_as_float(v.y & 0xFFFF0000u);
 }
 // Four from `at` of a row of any alignment and end: -infinity behind it.
 template <typename Tio>
 __device__ __forceinline__ void four(const Tio* z, int at, int V, float (&x)[4]) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) x[j] = at + j < V ? clean(ld_logit(z, at + j)) : -INFINITY;
+  for (int j = 0; j < 4; ++j) x[j] = at + j < V ? ld_logit(z, at + j) : -INFINITY;
 }
 
-// 2^(-y/8) for y in [0, 1): the Taylor polynomial about 0; its first omitted term is below 8e-14.  Exactly 1 at 0: rows of equal
-// logits have weights whose sums are exact, and so have u * Z between two of them.
+// 2^(-y/8) for y in [0, 1): the Taylor polynomial about 0; its first omitted term is below 8e-14.
 __device__ __forceinline__ double exp2_neg8(double y) {
   constexpr double kLn = -0.6931471805599453094 / 8;
   double p = kLn * kLn * kLn * kLn * kLn * kLn * kLn / 5040;
@@ -72,31 +74,41 @@ __device__ __forceinline__ double exp2_neg8(double y) {
   p = p * y + kLn;
   return p * y + 1.0;
 }
-// 2^(-i/8)
-__device__ __forceinline__ double eighth(int i) {
-  const double r[8] = {1.0, 0.91700404320467123174, 0.84089641525371454303, 0.77110541270397041180,
-                       0.70710678118654752440, 0.64841977732550483296, 0.59460355750136053336, 0.54525386633262882960};
-  double x = r[0];
-#pragma unroll
-  for (int j = 1; j < 8; ++j) x = i == j ? r[j] : x;
-  return x;
+// 2^-d for d >= 0 (NaN and beyond 2^-1074: 0): 2^-n times the Taylor polynomial of the rest, |rest| <= 1/2; its first omitted term
+// is below 3e-13.  Exactly 1 at 0: rows of equal logits have weights whose sums are exact, and so is u * Z between two of them.
+__device__ __forceinline__ double exp2_neg(double d) {
+  d = __builtin_fmin(d, 1100.0);
+  const double n = __builtin_rint(d), y = n - d;
+  constexpr double k1 = 0.6931471805599453094, k2 = k1 * k1 / 2, k3 = k2 * k1 / 3, k4 = k3 * k1 / 4, k5 = k4 * k1 / 5, k6 = k5 * k1 / 6,
+                   k7 = k6 * k1 / 7, k8 = k7 * k1 / 8, k9 = k8 * k1 / 9, k10 = k9 * k1 / 10;
+  double p = k10;
+  p = p * y + k9;
+  p = p * y + k8;
+  p = p * y + k7;
+  p = p * y + k6;
+  p = p * y + k5;
+  p = p * y + k4;
+  p = p * y + k3;
+  p = p * y + k2;
+  p = p * y + k1;
+  p = p * y + 1.0;
+  return __builtin_ldexp(p, -(int)n);
 }
 
-// How far a logit lies below the row's maximum, in eighths of an octave of its weight.
+// How far a logit lies below the row's maximum, and its weight.
 struct Scale {
   float zmax;
-  double c8;   // 8 log2(e) / T
-  __device__ __forceinline__ double dist8(float z) const { return z == zmax ? 0.0 : ((double)zmax - (double)z) * c8; }
+  double c;   // log2(e) / T
+  // in octaves of its weight
+  __device__ __forceinline__ double dist(float z) const {
+    if (zmax == INFINITY) return z == zmax ? 0.0 : INFINITY;
+    return ((double)zmax - (double)z) * c;
+  }
   __device__ __forceinline__ int bin(float z) const {
-    const double d = dist8(z);
+    const double d = dist(z) * 8.0;
     return d < (double)kLast ? (int)d : kLast;
   }
-  __device__ __forceinline__ double weight(float z) const {
-    const double d = dist8(z);
-    if (!(d < 8000.0)) return 0.0;
-    const int b = (int)d;
-    return ldexp(exp2_neg8(d - b) * eighth(b & 7), -(b >> 3));
-  }
+  __device__ __forceinline__ double weight(float z) const { return exp2_neg(dist(z)); }
   // the weight in units of 2^-50 of the maximum's (sums of kList of them fit)
   __device__ __forceinline__ u64 units(float z) const { return (u64)(weight(z) * 0x1p50 + 0.5); }
 };
@@ -104,7 +116,7 @@ struct Scale {
 __device__ __forceinline__ u64 mant8(double frac) {   // (adding 2^8 leaves units of 2^-44 in the last bits)
   return (u64)__double_as_longlong(exp2_neg8(frac) + 256.0) - 0x4070000000000000ull;
 }
-__device__ __forceinline__ double bin_unit(int bin) { return bin >= kLast ? 0.0 : ldexp(eighth(bin & 7), -44 - (bin >> 3)); }
+__device__ __forceinline__ double bin_unit(int bin) { return bin >= kLast ? 0.0 : exp2_neg((double)bin * 0.125 + 44.0); }
 
 template <class T>
 __device__ __forceinline__ T wave_sum(T v) {
@@ -146,7 +158,6 @@ struct Row {
   const Tio* z;
   int V, tid, lane, wave;
   bool vec;
-  Scale sc;
 
   // f(x, first index) for every four tokens of a strip of kStrip tokens, strip by strip of this wave's share, then
   // done(strip).  A whole strip's loads are under way together; they are not conditional, or the next would wait for the last.
@@ -267,7 +278,7 @@ __device__ void refine(Shared& s, const Scale& sc, int tid, int lane, int wave, 
       const uint32_t key = key_of(x);
       if (key < lo || key > hi || sc.bin(x) != bin) return;
       const int b = (int)((hi - key) >> shift);
-      const double d = sc.dist8(x);
+      const double d = 8.0 * sc.dist(x);
       atomicAdd(&s.cnt[b], 1u);
       if (bin < kLast) atomicAdd(&s.mass[b], mant8(d - bin));
     });
@@ -337,7 +348,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
   Shared& s = *reinterpret_cast<Shared*>(lds);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int row = blockIdx.x, V = a.V;
-  Row<Tio> rw{s, (const Tio*)a.z + (int64_t)row * a.ld, V, tid, lane, wave, false, {0.f, 0.0}};
+  Row<Tio> rw{s, (const Tio*)a.z + (int64_t)row * a.ld, V, tid, lane, wave, false};
   rw.vec = ((uintptr_t)rw.z & (4 * sizeof(Tio) - 1)) == 0;   // (a row whose four tokens do not start on their size goes one by one)
   const float temp = a.temperature[row];
   const int k = a.top_k ? a.top_k[row] : 0;
@@ -352,7 +363,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       best = fmaxf(best, x[j]);
-      valid += (unsigned)__popcll(__ballot(x[j] > -INFINITY));   // (of the wave)
+      valid += (unsigned)__popcll(__ballot(is_token(x[j])));   // (of the wave)
     }
   });
 #pragma unroll
@@ -382,7 +393,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
     }
     return;
   }
-  const Scale sc{best, 8.0 * 1.4426950408889634074 / (double)temp};
+  const Scale sc{best, 1.4426950408889634074 / (double)temp};
   const double min_w = mp > 0.f ? (double)mp : 0.0;
   const bool limit_k = k > 0 && (u64)k < valid, limit_p = p < 1.f;
 
@@ -395,7 +406,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
     rw.strips([&](const float (&x)[4], int) {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        if (x[j] > -INFINITY) atomicAdd(&s.cnt[sc.bin(x[j])], 1u);
+        if (is_token(x[j])) atomicAdd(&s.cnt[sc.bin(x[j])], 1u);
     });
     __syncthreads();
     find_bin(s, tid, lane, wave, 0, 0.0, s.cnt[tid], 0.0, Goal{(u64)k, INFINITY});
@@ -417,8 +428,8 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
     rw.strips([&](const float (&x)[4], int) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        if (!(x[j] > -INFINITY)) continue;
-        const double d = sc.dist8(x[j]);
+        if (!is_token(x[j])) continue;
+        const double d = 8.0 * sc.dist(x[j]);
         const int b = d < (double)kLast ? (int)d : kLast;
         atomicAdd(&s.cnt[b], 1u);
         if (b < kLast) atomicAdd(&s.mass[b], mant8(d - b));
@@ -456,15 +467,15 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
   const bool cut_needed = limit_k || limit_p;
   bool whole = (cut_needed || min_w > 0.0) && n_to <= kList;
   auto gather = [&](int a_bin, int b_bin) {
+    const double d_a = a_bin, d_b = b_bin == kLast ? INFINITY : b_bin + 1.0;
     __syncthreads();
     if (tid == 0) s.n_list = 0;
     __syncthreads();
     rw.strips([&](const float (&x)[4], int at) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        if (!(x[j] > -INFINITY)) continue;
-        const int b = sc.bin(x[j]);
-        if (b < a_bin || b > b_bin) continue;
+        const double d = 8.0 * sc.dist(x[j]);
+        if (!(is_token(x[j]) && d >= d_a && (d < d_b || d_b == INFINITY))) continue;
         const uint32_t e = atomicAdd(&s.n_list, 1u);
         if (e < kList) { s.list.z[e] = x[j]; s.list.i[e] = at + j; }
       }
@@ -483,7 +494,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
     rw.strips([&](const float (&x)[4], int at) {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        if (x[j] > -INFINITY) f(x[j], at + j);
+        if (is_token(x[j])) f(x[j], at + j);
     });
   };
 
@@ -519,7 +530,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
       s.mass[tid] = 0;
       __syncthreads();
       auto add = [&](float x, int) {
-        const double d = sc.dist8(x);
+        const double d = 8.0 * sc.dist(x);
         const int b = d < (double)kLast ? (int)d : kLast;
         if (b > bin_k) return;
         atomicAdd(&s.cnt[b], 1u);
@@ -565,13 +576,13 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
         u64 mine = 0, nb;
         double mb;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) mine += x[j] > -INFINITY && key_of(x[j]) == cut.key;
+        for (int j = 0; j < 4; ++j) mine += is_token(x[j]) && key_of(x[j]) == cut.key;
         block_scan(s, lane, wave, mine, 0.0, nb, mb);
         nb += seen;
         if (nb < ties && nb + mine >= ties) {
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            if (x[j] > -INFINITY && key_of(x[j]) == cut.key && ++nb == ties) s.index = at + j;
+            if (is_token(x[j]) && key_of(x[j]) == cut.key && ++nb == ties) s.index = at + j;
         }
         if (tid == kThreads - 1) s.n_at = nb < ties || mine == 0 ? nb + mine : ties;
         __syncthreads();
@@ -583,10 +594,9 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
       __syncthreads();
     }
   }
-  auto kept = [&](float x, int i) {   // (of a token above -infinity)
-    const uint32_t key = key_of(x);
-    return key > cut.key || (key == cut.key && i <= cut.limit);
-  };
+  const float z_cut = cut_needed ? of_key(cut.key) : kLeast;   // (no cut: all of the least are kept too)
+  const int limit = cut_needed ? cut.limit : 0x7FFFFFFF;
+  auto kept = [&](float x, int i) { return x > z_cut || (x == z_cut && i <= limit); };   // (false for NaN)
   const float u0 = a.u[row];
   const double u1 = u0 > 0.f ? (u0 < 1.f ? (double)u0 : 1.0) : 0.0;
 
@@ -616,18 +626,15 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
     if (target >= sum) target = sum - 1;   // (the last token with a weight)
     list_index(s, tid, lane, wave, n_list, V, target, val);
     if (tid == 0) {
-      const int i = s.index;
+      const int i = min(s.index, V - 1);
       a.tokens[row] = i;
-      if (a.prob) a.prob[row] = (float)(sc.weight(clean(ld_logit(rw.z, i))) / ((double)sum * 0x1p-50));
+      if (a.prob) a.prob[row] = (float)(sc.weight(ld_logit(rw.z, i)) / ((double)sum * 0x1p-50));
       if (a.n_kept) a.n_kept[row] = (int32_t)number;
     }
     return;
   }
-  auto weight = [&](float x, int i) -> double {   // negative: not kept
-    if (!(x > -INFINITY) || !kept(x, i)) return -1.0;
-    const double w = sc.weight(x);
-    return w >= min_w || x == sc.zmax ? w : -1.0;
-  };
+  // (a token that is not kept lies at the far end: its weight underflows)
+  auto weight = [&](float x, int i) { return exp2_neg(kept(x, i) ? sc.dist(x) : 1100.0); };
   const int strips = (V + kStrip - 1) / kStrip;
   u64 number = 0;
   double part = 0.0;
@@ -636,9 +643,14 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
       [&](const float (&x)[4], int at) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const double w = weight(x[j], at + j);
-          number += (unsigned)__popcll(__ballot(w >= 0.0));
-          part += w > 0.0 ? w : 0.0;
+          double w = weight(x[j], at + j);
+          bool in = kept(x[j], at + j);
+          if (min_w > 0.0) {
+            in = in && (w >= min_w || x[j] == sc.zmax);
+            w = in ? w : 0.0;
+          }
+          number += (unsigned)__popcll(__ballot(in));
+          part += w;
         }
       },
       [&](int st) {
@@ -665,7 +677,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
   }
   __syncthreads();
   const bool passed = s.bin != 0x7FFFFFFF;
-  const int at = passed ? s.bin : s.index;   // (the last strip with a weight if rounding leaves none)
+  const int at = passed ? s.bin : max(s.index, 0);   // (the last strip with a weight if rounding leaves none)
   if (tid == at) s.m_before = mb;
   __syncthreads();
   if (wave != 0) return;
@@ -680,7 +692,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       w[j] = weight(x[j], first + j);
-      if (!(w[j] > 0.0)) w[j] = 0.0;
+      if (!(w[j] >= min_w || x[j] == sc.zmax)) w[j] = 0.0;
       run += w[j];
     }
     const double inc = wave_scan(run, lane);
