@@ -5,14 +5,20 @@
 //
 // Sampling without a sort.  With the order "logit descending, index ascending" all three filters keep a prefix of a
 // row's tokens, so what has to be found is the prefix's last token, never the order itself.  Weights are w = 2^-d,
-// d = (M - z) log2(e) / T >= 0 in double; a token falls into bin floor(8 d), and a histogram of counts and weights over the
-// bins tells in which bin the prefix ends.  Sums of weights are sums of 64-bit integers wherever threads add in any order, so
-// they do not depend on it.  The bin where the prefix ends is cut again by the bits of its logits until one value is left,
-// and equal logits are kept by ascending index.  The draw is a search in the kept tokens' running sum by index.
+// d = (M - z) log2(e) / T >= 0 in double; sums of weights are sums of 64-bit integers wherever threads add in any order, so
+// they do not depend on it.
+//   top-k    the k-th largest of the threads' own maxima bounds the k-th largest token from below: the tokens above it, a
+//            few more than k, are gathered into LDS and no other needs an exponential.  (More than kList of them, or k beyond
+//            the threads: a histogram of counts finds the bound.)
+//   top-p    a histogram of weights over bins of an eighth of an octave finds the bin in which the prefix ends; inside a bin
+//            the weights' mantissas add up as integers, and their sum tells the number of tokens within 5 %.
+//   min-p    a comparison.
+// Up to kThreads gathered tokens are compared each with each: ranks, weights before them and running sums by index in one
+// sweep.  More of them, up to kList: the bin is cut again by the bits of its logits until one value is left, and equal logits
+// are kept by ascending index.  A prefix of more than kList tokens stays in memory: only the last bin's tokens are gathered, and
+// the draw reads the row again for its running sum.
 //
-// One workgroup of 16 waves per row.  A row is read once for its maximum, once for the histogram (counts alone take no
-// exponential: a top-k row needs none for the tokens it drops), and once to gather the tokens that matter into LDS, where
-// the rest happens; only a row that keeps more than kList tokens reads them a third time, for its running sum.
+// One workgroup of 16 waves per row; what bounds it is the double-precision arithmetic, 20 operations for a weight.
 #include "zo_device.hpp"
 #include "zo_internal.hpp"
 
@@ -62,11 +68,12 @@ __device__ __forceinline__ void four(const Tio* z, int at, int V, float (&x)[4])
   for (int j = 0; j < 4; ++j) x[j] = at + j < V ? ld_logit(z, at + j) : -INFINITY;
 }
 
-// 2^(-y/8) for y in [0, 1): the Taylor polynomial about 0; its first omitted term is below 8e-14.
-__device__ __forceinline__ double exp2_neg8(double y) {
-  constexpr double kLn = -0.6931471805599453094 / 8;
-  double p = kLn * kLn * kLn * kLn * kLn * kLn * kLn / 5040;
-  p = p * y + kLn * kLn * kLn * kLn * kLn * kLn / 720;
+// Adding it leaves the nearest integer in the low word.
+constexpr double kMagic = 6755399441055744.0;   // 1.5 * 2^52
+// 2^(y/8) for |y| <= 1/2: the Taylor polynomial; its first omitted term is below 6e-14.
+__device__ __forceinline__ double exp2_eighth(double y) {
+  constexpr double kLn = 0.6931471805599453094 / 8;
+  double p = kLn * kLn * kLn * kLn * kLn * kLn / 720;
   p = p * y + kLn * kLn * kLn * kLn * kLn / 120;
   p = p * y + kLn * kLn * kLn * kLn / 24;
   p = p * y + kLn * kLn * kLn / 6;
@@ -74,11 +81,10 @@ __device__ __forceinline__ double exp2_neg8(double y) {
   p = p * y + kLn;
   return p * y + 1.0;
 }
-// 2^-d for d >= 0 (NaN and beyond 2^-1074: 0): 2^-n times the Taylor polynomial of the rest, |rest| <= 1/2; its first omitted term
-// is below 3e-13.  Exactly 1 at 0: rows of equal logits have weights whose sums are exact, and so is u * Z between two of them.
-__device__ __forceinline__ double exp2_neg(double d) {
-  d = __builtin_fmin(d, 1100.0);
-  const double n = __builtin_rint(d), y = n - d;
+// 2^(-diff c) for diff c in [0, 1000]: 2^-n times the Taylor polynomial of the rest, |rest| <= 1/2; its first omitted term is
+// below 3e-13.  Exactly 1 at 0: rows of equal logits have weights whose sums are exact, and so is u * Z between two of them.
+__device__ __forceinline__ double exp2_neg(double diff, double c) {
+  const double t = __builtin_fma(diff, c, kMagic), y = __builtin_fma(-diff, c, t - kMagic);
   constexpr double k1 = 0.6931471805599453094, k2 = k1 * k1 / 2, k3 = k2 * k1 / 3, k4 = k3 * k1 / 4, k5 = k4 * k1 / 5, k6 = k5 * k1 / 6,
                    k7 = k6 * k1 / 7, k8 = k7 * k1 / 8, k9 = k8 * k1 / 9, k10 = k9 * k1 / 10;
   double p = k10;
@@ -92,31 +98,48 @@ __device__ __forceinline__ double exp2_neg(double d) {
   p = p * y + k2;
   p = p * y + k1;
   p = p * y + 1.0;
-  return __builtin_ldexp(p, -(int)n);
+  // (the exponent takes n off by itself: p is next to 1 and the result no smaller than 2^-1001)
+  return __hiloint2double(__double2hiint(p) - (__double2loint(t) << 20), __double2loint(p));
 }
 
 // How far a logit lies below the row's maximum, and its weight.
 struct Scale {
   float zmax;
-  double c;   // log2(e) / T
-  // in octaves of its weight
-  __device__ __forceinline__ double dist(float z) const {
-    if (zmax == INFINITY) return z == zmax ? 0.0 : INFINITY;
-    return ((double)zmax - (double)z) * c;
+  double c;        // log2(e) / T
+  float far_bin;   // below it lies the last bin (2^-127.8 of the largest weight)
+  float far;       // below it a weight is none (2^-1000)
+
+  __device__ __forceinline__ Scale(float zmax, float temp) : zmax(zmax), c(1.4426950408889634074 / (double)temp) {
+    far_bin = below(127.8, true);
+    far = below(1000.0, true);
   }
+  // The logit whose weight is 2^-octaves of the largest: the next one above that or the next below.
+  __device__ __forceinline__ float below(double octaves, bool above) const {
+    const double z = (double)zmax - octaves / c;
+    if (!(z > (double)kLeast)) return kLeast;
+    const float f = (float)z;
+    return above ? ((double)f < z ? nextafterf(f, INFINITY) : f) : ((double)f > z ? nextafterf(f, -INFINITY) : f);
+  }
+  __device__ __forceinline__ double diff(float z) const { return (double)zmax - (double)z; }
   __device__ __forceinline__ int bin(float z) const {
-    const double d = dist(z) * 8.0;
-    return d < (double)kLast ? (int)d : kLast;
+    if (!(z >= far_bin)) return kLast;
+    return (int)min((uint32_t)__double2loint(__builtin_fma(diff(z), 8.0 * c, kMagic)), (uint32_t)kLast - 1);
   }
-  __device__ __forceinline__ double weight(float z) const { return exp2_neg(dist(z)); }
-  // the weight in units of 2^-50 of the maximum's (sums of kList of them fit)
-  __device__ __forceinline__ u64 units(float z) const { return (u64)(weight(z) * 0x1p50 + 0.5); }
+  // bin and mantissa of a logit from far_bin on: its weight is mant * bin_unit(bin)
+  __device__ __forceinline__ int bin(float z, u64& mant) const {
+    const double d = diff(z), t = __builtin_fma(d, 8.0 * c, kMagic), y = __builtin_fma(-d, 8.0 * c, t - kMagic);
+    // (adding 2^8 leaves units of 2^-44 in the last bits: sums of kMaxVocab of them fit into 64)
+    mant = (u64)__double_as_longlong(exp2_eighth(y) + 256.0) - 0x4070000000000000ull;
+    return (int)min((uint32_t)__double2loint(t), (uint32_t)kLast - 1);
+  }
+  __device__ __forceinline__ double weight(float z) const { return z >= far ? exp2_neg(diff(z), c) : 0.0; }
+  // a weight in units of 2^-50 of the largest (sums of kList of them fit), at least one
+  __device__ __forceinline__ static u64 units(double w) {
+    const u64 n = (u64)(w * 0x1p50 + 0.5);
+    return n ? n : (u64)(w > 0.0);
+  }
 };
-// A weight is mant * bin_unit(bin) with mant in units of 2^-44: sums of kMaxVocab mantissas fit into 64 bits.
-__device__ __forceinline__ u64 mant8(double frac) {   // (adding 2^8 leaves units of 2^-44 in the last bits)
-  return (u64)__double_as_longlong(exp2_neg8(frac) + 256.0) - 0x4070000000000000ull;
-}
-__device__ __forceinline__ double bin_unit(int bin) { return bin >= kLast ? 0.0 : exp2_neg((double)bin * 0.125 + 44.0); }
+__device__ __forceinline__ double bin_unit(int bin) { return bin >= kLast ? 0.0 : exp2_neg((double)bin, 0.125) * 0x1p-44; }
 
 template <class T>
 __device__ __forceinline__ T wave_sum(T v) {
@@ -252,7 +275,7 @@ struct Cut {
 // bin.  n0, m0: what lies before the bin.  Leaves the key in s.lo, the number of equals to keep in s.n_at, the kept tokens'
 // count in s.n_before + s.n_at and their weight in s.total.
 template <class Each>
-__device__ void refine(Shared& s, const Scale& sc, int tid, int lane, int wave, int bin, u64 n0, double m0, const Goal& goal, Each each) {
+__device__ __forceinline__ void refine(Shared& s, const Scale& sc, int tid, int lane, int wave, int bin, u64 n0, double m0, const Goal& goal, Each each) {
   const double unit = bin_unit(bin);
   __syncthreads();
   if (tid == 0) { s.lo = 0xFFFFFFFFu; s.hi = 0; }
@@ -278,9 +301,12 @@ __device__ void refine(Shared& s, const Scale& sc, int tid, int lane, int wave, 
       const uint32_t key = key_of(x);
       if (key < lo || key > hi || sc.bin(x) != bin) return;
       const int b = (int)((hi - key) >> shift);
-      const double d = 8.0 * sc.dist(x);
       atomicAdd(&s.cnt[b], 1u);
-      if (bin < kLast) atomicAdd(&s.mass[b], mant8(d - bin));
+      if (bin < kLast) {
+        u64 mant;
+        sc.bin(x, mant);
+        atomicAdd(&s.mass[b], mant);
+      }
     });
     __syncthreads();
     find_bin(s, tid, lane, wave, n0, m0, s.cnt[tid], (double)s.mass[tid] * unit, goal);
@@ -312,7 +338,7 @@ __device__ void refine(Shared& s, const Scale& sc, int tid, int lane, int wave, 
 
 // The lowest index at which the running sum by index of val(z, index) over a list exceeds `target` (below the whole sum): s.index.
 template <class Val>
-__device__ void list_index(Shared& s, int tid, int lane, int wave, int n, int V, u64 target, Val val) {
+__device__ __forceinline__ void list_index(Shared& s, int tid, int lane, int wave, int n, int V, u64 target, Val val) {
   int shift = 0;
   while (((V - 1) >> shift) >= kBins) ++shift;   // (at most 9)
   int first = 0;
@@ -342,6 +368,62 @@ __device__ void list_index(Shared& s, int tid, int lane, int wave, int n, int V,
   __syncthreads();
 }
 
+// The index of the n-th (from 0) token of the row for which is(z), which there is: s.index.  Counts by strips, then the strip.
+template <typename Tio, class Is>
+__device__ __forceinline__ void nth_index(const Row<Tio>& rw, u64 n, Is is) {
+  Shared& s = rw.s;
+  const int strips = (rw.V + kStrip - 1) / kStrip;
+  uint32_t c = 0;
+  __syncthreads();
+  rw.strips(
+      [&](const float (&x)[4], int) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c += (unsigned)__popcll(__ballot(is(x[j])));
+      },
+      [&](int st) {
+        if (rw.lane == 0) s.cnt[st] = c;
+        c = 0;
+      });
+  __syncthreads();
+  const u64 mine = rw.tid < strips ? s.cnt[rw.tid] : 0;
+  u64 nb;
+  double mb;
+  block_scan(s, rw.lane, rw.wave, mine, 0.0, nb, mb);
+  if (rw.tid == 0) { s.bin = 0; s.index = 0; s.n_before = 0; }
+  __syncthreads();
+  if (nb <= n && nb + mine > n) { s.bin = rw.tid; s.n_before = nb; }
+  __syncthreads();
+  if (rw.wave == 0) {
+    u64 seen = s.n_before;
+    for (int u = 0; u < kPieces; ++u) {
+      float x[4];
+      const int at = s.bin * kStrip + u * (4 * kWave) + rw.lane * 4;
+      four(rw.z, at, rw.V, x);
+      int here = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) here += is(x[j]);
+      const int inc = wave_scan(here, rw.lane);
+      u64 b = seen + (u64)(inc - here);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (is(x[j]) && b++ == n) s.index = at + j;
+      seen += (u64)__shfl(inc, kWave - 1);
+    }
+  }
+  __syncthreads();
+}
+
+// Sum over the workgroup, for every thread.
+__device__ __forceinline__ u64 block_sum(Shared& s, int lane, int wave, u64 v) {
+  v = wave_sum(v);
+  __syncthreads();
+  if (lane == 0) s.wave_n[wave] = v;
+  __syncthreads();
+  u64 n = 0;
+  for (int w = 0; w < kWaves; ++w) n += s.wave_n[w];
+  return n;
+}
+
 template <typename Tio>
 __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -354,7 +436,14 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
   const int k = a.top_k ? a.top_k[row] : 0;
   const float p = a.top_p ? a.top_p[row] : 1.f;
   const float mp = a.min_p ? a.min_p[row] : 0.f;
+  const float u0 = a.u[row];
+  const double u1 = u0 > 0.f ? (u0 < 1.f ? (double)u0 : 1.0) : 0.0;
   const bool greedy = !(temp > 0.f);
+  auto answer = [&](int token, double prob, u64 number) __attribute__((always_inline)) {
+    a.tokens[row] = token;
+    if (a.prob) a.prob[row] = (float)prob;
+    if (a.n_kept) a.n_kept[row] = (int32_t)number;
+  };
 
   // ---- maximum, tokens above -infinity
   float best = -INFINITY;
@@ -366,275 +455,301 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
       valid += (unsigned)__popcll(__ballot(is_token(x[j])));   // (of the wave)
     }
   });
+  const float own = best;
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) best = fmaxf(best, __shfl_xor(best, o));
   if (lane == 0) { s.wave_z[wave] = best; s.wave_n[wave] = valid; }
-  if (tid == 0) { s.index = 0x7FFFFFFF; s.n_list = 0; }
+  if (tid == 0) { s.index = 0; s.n_list = 0; }
   s.cnt[tid] = 0;
   s.mass[tid] = 0;
   __syncthreads();
   valid = 0;
   for (int w = 0; w < kWaves; ++w) { best = fmaxf(best, s.wave_z[w]); valid += s.wave_n[w]; }
-  if (valid == 0 || greedy) {
-    if (valid) {   // the lowest index with the maximum
-      int at = 0x7FFFFFFF;
-      rw.strips([&](const float (&x)[4], int i) {
-#pragma unroll
-        for (int j = 3; j >= 0; --j)
-          if (x[j] == best) at = min(at, i + j);
-      });
-      atomicMin(&s.index, at);
-      __syncthreads();
-    }
-    if (tid == 0) {
-      a.tokens[row] = valid ? s.index : -1;
-      if (a.prob) a.prob[row] = valid ? 1.f : 0.f;
-      if (a.n_kept) a.n_kept[row] = valid ? 1 : 0;
-    }
+  if (valid == 0) {
+    if (tid == 0) answer(-1, 0.0, 0);
     return;
   }
-  const Scale sc{best, 1.4426950408889634074 / (double)temp};
-  const double min_w = mp > 0.f ? (double)mp : 0.0;
-  const bool limit_k = k > 0 && (u64)k < valid, limit_p = p < 1.f;
+  const bool limit_k = k > 0 && (u64)k < valid, limit_p = p < 1.f, limit_m = mp > 0.f;
+  const double min_w = limit_m ? (double)mp : 0.0;
+  if (greedy || best == INFINITY) {
+    // the first of the largest, or one of those at +infinity: of weight 1 each, the others have none
+    u64 n = 0, number = 1;
+    double prob = 1.0;
+    __syncthreads();
+    if (!greedy) {
+      u64 mine = 0;
+      rw.strips([&](const float (&x)[4], int) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) mine += x[j] == best;
+      });
+      const u64 at_top = block_sum(s, lane, wave, mine), first_k = limit_k ? (u64)k : valid;
+      const u64 mass_k = first_k < at_top ? first_k : at_top;
+      number = first_k;
+      if (limit_p) {
+        const double c = ceil((double)p * (double)mass_k);
+        number = c < 1.0 ? 1 : c < (double)mass_k ? (u64)c : mass_k;
+      }
+      if (limit_m && number > at_top) number = at_top;
+      const u64 drawn = number < at_top ? number : at_top;
+      n = (u64)(u1 * (double)drawn);
+      if (n >= drawn) n = drawn - 1;
+      prob = 1.0 / (double)drawn;
+      __syncthreads();
+    }
+    nth_index(rw, n, [&](float x) { return x == best; });
+    if (tid == 0) answer(s.index, prob, number);
+    return;
+  }
+  const Scale sc(best, temp);
+  auto weight = [&](float x) { return sc.weight(x); };
+  auto by_min = [&](float x, double w) { return w >= min_w || x == sc.zmax; };
 
-  // ---- the bins at which the prefix may end.  Tokens of bins [from, to] are gathered; those before `from` are kept.
-  int to = kLast, from = 0, bin_k = kLast;
-  u64 n_k = valid, nb_k = 0;          // tokens that top-k leaves; tokens before its bin
-  double mb_k = 0.0, z_all = 0.0;
-  u64 n_to = valid;                   // tokens of bins [0, to]
+  // ---- the tokens of bins 0 .. `to` hold the prefix; n_to of them, about
+  int to = kLast;
+  double n_to = (double)valid;
+  // bin of the k-th largest of what add(f) passes to f
   if (limit_k) {
+    const bool few = k <= kThreads / 2;
+    if (few) {
+      if (is_token(own)) atomicAdd(&s.cnt[sc.bin(own)], 1u);
+    } else {
+      rw.strips([&](const float (&x)[4], int) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (is_token(x[j])) atomicAdd(&s.cnt[sc.bin(x[j])], 1u);
+      });
+    }
+    __syncthreads();
+    // (fewer than k threads with a token: the last bin in use, and then every bin)
+    find_bin(s, tid, lane, wave, 0, 0.0, s.cnt[tid], 0.0, Goal{(u64)k, INFINITY});
+    to = s.n_before + s.n_at >= (u64)k ? s.bin : kLast;
+    n_to = few ? 0.0 : (double)(s.n_before + s.n_at);   // (0: not known, the gathering tells)
+    __syncthreads();
+  }
+  // weights of all bins, for a limit on weight among more tokens than fit in LDS
+  double z_all = 0.0, m_to = 0.0;
+  int bin_p = -1;
+  auto weigh = [&]() __attribute__((always_inline)) {
+    __syncthreads();
+    s.mass[tid] = 0;
+    __syncthreads();
     rw.strips([&](const float (&x)[4], int) {
+      u64 mant[4];
+      int b[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) b[j] = sc.bin(x[j], mant[j]);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        if (is_token(x[j])) atomicAdd(&s.cnt[sc.bin(x[j])], 1u);
+        if (x[j] >= sc.far_bin) atomicAdd(&s.mass[b[j]], mant[j]);
     });
     __syncthreads();
-    find_bin(s, tid, lane, wave, 0, 0.0, s.cnt[tid], 0.0, Goal{(u64)k, INFINITY});
-    bin_k = to = s.bin;
-    nb_k = s.n_before;
-    n_to = s.n_before + s.n_at;
-    n_k = (u64)k;
-    __syncthreads();
-  }
-  // the weights of the bins, where a limit on weight follows and the tokens do not all fit in LDS
-  const bool weigh = limit_p && (!limit_k || n_to > kList);
-  int bin_p = -1;
-  u64 nb_p = 0;
-  double mb_p = 0.0;
-  if (weigh) {
-    __syncthreads();
-    s.cnt[tid] = 0;
-    __syncthreads();
-    rw.strips([&](const float (&x)[4], int) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (!is_token(x[j])) continue;
-        const double d = 8.0 * sc.dist(x[j]);
-        const int b = d < (double)kLast ? (int)d : kLast;
-        atomicAdd(&s.cnt[b], 1u);
-        if (b < kLast) atomicAdd(&s.mass[b], mant8(d - b));
-      }
-    });
-    __syncthreads();
+  };
+  if (limit_p && !limit_k) {
+    weigh();
+    const u64 sum = s.mass[tid];
+    const double mass = (double)sum * bin_unit(tid);
     u64 nb;
     double mb;
-    const u64 cnt = s.cnt[tid];
-    const double mass = (double)s.mass[tid] * bin_unit(tid);
-    block_scan(s, lane, wave, cnt, mass, nb, mb);
+    block_scan(s, lane, wave, sum, mass, nb, mb);
     if (tid == kLast) s.total = mb + mass;
-    if (tid == bin_k) { s.m_before = mb; s.m_at = mass; }
     __syncthreads();
     z_all = s.total;
-    mb_k = s.m_before;
-    // Z_k lies between the weight before top-k's bin and the weight with it
-    const double lo = limit_k ? s.m_before : z_all;
+    find_bin(s, tid, lane, wave, 0, 0.0, (uint32_t)(sum > 0), mass, Goal{~0ull, (double)p * z_all});
+    bin_p = to = s.bin;
+    m_to = s.m_before;
+    if (tid == to) s.total = (double)(nb + sum) * (0x1p-44 * 1.05);
     __syncthreads();
-    find_bin(s, tid, lane, wave, 0, 0.0, cnt, mass, Goal{~0ull, (double)p * lo});
-    bin_p = s.bin;
-    nb_p = s.n_before;
-    mb_p = s.m_before;
-    const u64 with = s.n_before + s.n_at;
-    if (!limit_k) { to = bin_p; n_to = with; }
+    n_to = s.total;
     __syncthreads();
   }
-  if (min_w > 0.0 && !limit_k && !limit_p) {   // (one bin more than the logarithm says: its rounding must not matter)
-    const double d = -log2(min_w) * 8.0;
-    to = d < (double)(kLast - 2) ? (d > 0.0 ? (int)d + 1 : 1) : kLast;
-    n_to = 0;   // (not known: the gathering tells)
+  if (limit_m && !limit_k && !limit_p) {   // (a bin more than the logarithm says: roundings must not matter)
+    const double d = -log2(min_w) * 8.0 + 2.0;
+    to = d < (double)(kLast - 1) ? (d > 1.0 ? (int)d : 1) : kLast;
+    n_to = 0.0;
   }
 
   // ---- the tokens of the prefix in LDS, if they fit
   const bool cut_needed = limit_k || limit_p;
-  bool whole = (cut_needed || min_w > 0.0) && n_to <= kList;
-  auto gather = [&](int a_bin, int b_bin) {
-    const double d_a = a_bin, d_b = b_bin == kLast ? INFINITY : b_bin + 1.0;
+  auto gather = [&](int a_bin, int b_bin) __attribute__((always_inline)) {
+    // (a comparison keeps most tokens out, with a bin to spare for its rounding)
+    const float least = b_bin >= kLast - 2 ? kLeast : sc.below((b_bin + 1.5) * 0.125, false);
     __syncthreads();
     if (tid == 0) s.n_list = 0;
     __syncthreads();
     rw.strips([&](const float (&x)[4], int at) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const double d = 8.0 * sc.dist(x[j]);
-        if (!(is_token(x[j]) && d >= d_a && (d < d_b || d_b == INFINITY))) continue;
+        if (!(x[j] >= least)) continue;
+        const int b = sc.bin(x[j]);
+        if (b < a_bin || b > b_bin) continue;
         const uint32_t e = atomicAdd(&s.n_list, 1u);
         if (e < kList) { s.list.z[e] = x[j]; s.list.i[e] = at + j; }
       }
     });
     __syncthreads();
   };
+  bool whole = (cut_needed || limit_m) && n_to <= (double)kList;
   if (whole) {
     gather(0, to);
     whole = s.n_list <= kList;
   }
   int n_list = whole ? (int)s.n_list : 0;
-  auto each_listed = [&](auto f) {
+
+  // ---- few tokens: each with each
+  if (whole && n_list <= kThreads) {
+    const bool mine = tid < n_list;
+    const float x = mine ? s.list.z[tid] : 0.f;
+    const int i = mine ? s.list.i[tid] : 0;
+    const double w = mine ? weight(x) : 0.0;
+    const u64 un = Scale::units(w);
+    s.mass[tid] = un;
+    __syncthreads();
+    bool in = mine;
+    if (cut_needed) {
+      u64 before = 0;
+      uint32_t rank = 0;
+      if (wave * kWave < n_list) {
+        for (int e = 0; e < n_list; ++e) {
+          const float y = s.list.z[e];
+          const bool first = y > x || (y == x && s.list.i[e] < i);
+          rank += first;
+          before += first ? s.mass[e] : 0;
+        }
+      }
+      if (limit_k) in = in && rank < (uint32_t)k;
+      if (limit_p) {
+        const double z_k = limit_k ? (double)block_sum(s, lane, wave, in ? un : 0) * 0x1p-50 : z_all;
+        in = in && (rank == 0 || (double)before * 0x1p-50 < (double)p * z_k);
+      }
+    }
+    in = in && by_min(x, w);
+    const u64 sum = block_sum(s, lane, wave, in ? un : 0);
+    const u64 number = block_sum(s, lane, wave, (u64)in);
+    s.mass[tid] = in ? un : 0;
+    if (tid == 0) s.hi = 0x7FFFFFFFu;
+    __syncthreads();
+    u64 target = (u64)(u1 * (double)sum);
+    if (target >= sum) target = sum - 1;   // (the last token with a weight)
+    if (wave * kWave < n_list) {
+      u64 upto = 0;
+      for (int e = 0; e < n_list; ++e) upto += s.list.i[e] <= i ? s.mass[e] : 0;
+      if (in && upto > target) atomicMin(&s.hi, (uint32_t)i);
+    }
+    __syncthreads();
+    if (in && (uint32_t)i == s.hi) answer(i, w / ((double)sum * 0x1p-50), number);
+    return;
+  }
+
+  auto each_listed = [&](auto f) __attribute__((always_inline)) {
     for (int e = tid; e < n_list; e += kThreads) f(s.list.z[e], s.list.i[e]);
   };
-  auto each_token = [&](auto f) {
+  auto each_token = [&](auto f) __attribute__((always_inline)) {
     rw.strips([&](const float (&x)[4], int at) {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         if (is_token(x[j])) f(x[j], at + j);
     });
   };
+  // counts and weights of the bins 0 .. `to`
+  auto histogram = [&](auto each) __attribute__((always_inline)) {
+    __syncthreads();
+    s.cnt[tid] = 0;
+    s.mass[tid] = 0;
+    __syncthreads();
+    each([&](float x, int) {
+      const int b = sc.bin(x);
+      if (b > to) return;
+      atomicAdd(&s.cnt[b], 1u);
+      if (b == kLast) return;
+      u64 mant;
+      sc.bin(x, mant);
+      atomicAdd(&s.mass[b], mant);
+    });
+    __syncthreads();
+  };
 
   // ---- the cut: by count, then by weight among what that left
-  Cut cut{0u, 0x7FFFFFFF};   // keeps everything
+  Cut cut{0u, 0x7FFFFFFF};
   u64 ties = 0;
   if (limit_k) {
-    const Goal goal{n_k, INFINITY};
-    if (whole && !weigh) {
-      // (the weights before the bin are those of the list)
-      u64 u = 0;
-      each_listed([&](float x, int) { u += sc.bin(x) < bin_k ? sc.units(x) : 0; });
-      u64 nb;
-      double mb;
-      block_scan(s, lane, wave, u, 0.0, nb, mb);
-      if (tid == kThreads - 1) s.m_before = (double)(nb + u) * 0x1p-50;
-      __syncthreads();
-      mb_k = s.m_before;
-      __syncthreads();
-    }
-    if (whole) refine(s, sc, tid, lane, wave, bin_k, nb_k, mb_k, goal, each_listed);
-    else refine(s, sc, tid, lane, wave, bin_k, nb_k, mb_k, goal, each_token);
-    cut.key = s.lo;
-    ties = s.n_at;
-    z_all = s.total;
-    __syncthreads();
-  }
-  if (limit_p) {
-    const Goal goal{n_k, (double)p * z_all};
-    // the bin: among those of the list, or of the histogram (its counts and weights have been overwritten if top-k came before)
-    if (limit_k) {
-      s.cnt[tid] = 0;
-      s.mass[tid] = 0;
-      __syncthreads();
-      auto add = [&](float x, int) {
-        const double d = 8.0 * sc.dist(x);
-        const int b = d < (double)kLast ? (int)d : kLast;
-        if (b > bin_k) return;
-        atomicAdd(&s.cnt[b], 1u);
-        if (b < kLast) atomicAdd(&s.mass[b], mant8(d - b));
-      };
-      if (whole) each_listed(add);
-      else each_token(add);
-      __syncthreads();
-      find_bin(s, tid, lane, wave, 0, 0.0, s.cnt[tid], (double)s.mass[tid] * bin_unit(tid), goal);
-      bin_p = s.bin;
-      nb_p = s.n_before;
-      mb_p = s.m_before;
-      __syncthreads();
-    }
-    if (whole) {
-      refine(s, sc, tid, lane, wave, bin_p, nb_p, mb_p, goal, each_listed);
-    } else {
-      gather(bin_p, bin_p);
-      if (s.n_list <= kList) {
-        n_list = (int)s.n_list;
-        refine(s, sc, tid, lane, wave, bin_p, nb_p, mb_p, goal, each_listed);
-      } else {
-        refine(s, sc, tid, lane, wave, bin_p, nb_p, mb_p, goal, each_token);
+    const Goal by_count{(u64)k, INFINITY};
+    auto cut_k = [&](auto each) __attribute__((always_inline)) {
+      histogram(each);
+      const uint32_t cnt = s.cnt[tid];
+      const double mass = (double)s.mass[tid] * bin_unit(tid);
+      find_bin(s, tid, lane, wave, 0, 0.0, cnt, mass, by_count);
+      const int bin_k = s.bin;
+      const u64 nb = s.n_before;
+      const double mb = s.m_before;
+      refine(s, sc, tid, lane, wave, bin_k, nb, mb, by_count, each);
+      cut.key = s.lo;
+      ties = s.n_at;
+      if (limit_p) {
+        const Goal by_both{(u64)k, (double)p * s.total};
+        histogram(each);
+        find_bin(s, tid, lane, wave, 0, 0.0, s.cnt[tid], (double)s.mass[tid] * bin_unit(tid), by_both);
+        const int b = s.bin;
+        const u64 nb_p = s.n_before;
+        const double mb_p = s.m_before;
+        refine(s, sc, tid, lane, wave, b, nb_p, mb_p, by_both, each);
+        cut.key = s.lo;
+        ties = s.n_at;
       }
+    };
+    if (whole) cut_k(each_listed);
+    else cut_k(each_token);
+  } else if (limit_p) {
+    const Goal by_mass{~0ull, (double)p * z_all};
+    if (!whole) {
+      gather(bin_p, bin_p);
+      n_list = s.n_list <= kList ? (int)s.n_list : 0;
     }
+    // (what the counts before the bin are does not matter)
+    if (whole || n_list > 0) refine(s, sc, tid, lane, wave, bin_p, 0, m_to, by_mass, each_listed);
+    else refine(s, sc, tid, lane, wave, bin_p, 0, m_to, by_mass, each_token);
     cut.key = s.lo;
     ties = s.n_at;
-    __syncthreads();
   }
+  __syncthreads();
   // ---- equal logits at the cut are kept by ascending index
   if (cut_needed) {
-    if (whole) {
+    if (whole || (!limit_k && n_list > 0))
       list_index(s, tid, lane, wave, n_list, V, ties - 1, [&](float x, int) { return (u64)(key_of(x) == cut.key); });
-      cut.limit = s.index;
-      __syncthreads();
-    } else {
-      // four tokens of every thread at a time, in order
-      u64 seen = 0;
-      for (int first = 0; first < V; first += 4 * kThreads) {
-        float x[4];
-        const int at = first + tid * 4;
-        four(rw.z, at, V, x);
-        u64 mine = 0, nb;
-        double mb;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) mine += is_token(x[j]) && key_of(x[j]) == cut.key;
-        block_scan(s, lane, wave, mine, 0.0, nb, mb);
-        nb += seen;
-        if (nb < ties && nb + mine >= ties) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (is_token(x[j]) && key_of(x[j]) == cut.key && ++nb == ties) s.index = at + j;
-        }
-        if (tid == kThreads - 1) s.n_at = nb < ties || mine == 0 ? nb + mine : ties;
-        __syncthreads();
-        seen = s.n_at;
-        __syncthreads();
-        if (seen >= ties) break;
-      }
-      cut.limit = s.index;
-      __syncthreads();
-    }
+    else
+      nth_index(rw, ties - 1, [&](float x) { return is_token(x) && key_of(x) == cut.key; });
+    cut.limit = s.index;
+    __syncthreads();
   }
   const float z_cut = cut_needed ? of_key(cut.key) : kLeast;   // (no cut: all of the least are kept too)
-  const int limit = cut_needed ? cut.limit : 0x7FFFFFFF;
+  const int limit = cut.limit;
   auto kept = [&](float x, int i) { return x > z_cut || (x == z_cut && i <= limit); };   // (false for NaN)
-  const float u0 = a.u[row];
-  const double u1 = u0 > 0.f ? (u0 < 1.f ? (double)u0 : 1.0) : 0.0;
 
   // ---- the draw
   if (whole) {
-    auto val = [&](float x, int i) -> u64 {
+    auto val = [&](float x, int i) __attribute__((always_inline)) -> u64 {
       if (!kept(x, i)) return 0;
-      const double w = sc.weight(x);
-      return w >= min_w || x == sc.zmax ? (u64)(w * 0x1p50 + 0.5) : 0;
+      const double w = weight(x);
+      return by_min(x, w) ? Scale::units(w) : 0;
     };
     u64 sum = 0, number = 0;
     each_listed([&](float x, int i) {
       if (!kept(x, i)) return;
-      const double w = sc.weight(x);
-      if (!(w >= min_w || x == sc.zmax)) return;
+      const double w = weight(x);
+      if (!by_min(x, w)) return;
       ++number;
-      sum += (u64)(w * 0x1p50 + 0.5);
+      sum += Scale::units(w);
     });
-    sum = wave_sum(sum);
-    number = wave_sum(number);
-    __syncthreads();
-    if (lane == 0) { s.wave_n[wave] = sum; s.mass[wave] = number; }
-    __syncthreads();
-    sum = number = 0;
-    for (int w = 0; w < kWaves; ++w) { sum += s.wave_n[w]; number += s.mass[w]; }
+    sum = block_sum(s, lane, wave, sum);
+    number = block_sum(s, lane, wave, number);
     u64 target = (u64)(u1 * (double)sum);
     if (target >= sum) target = sum - 1;   // (the last token with a weight)
     list_index(s, tid, lane, wave, n_list, V, target, val);
     if (tid == 0) {
       const int i = min(s.index, V - 1);
-      a.tokens[row] = i;
-      if (a.prob) a.prob[row] = (float)(sc.weight(ld_logit(rw.z, i)) / ((double)sum * 0x1p-50));
-      if (a.n_kept) a.n_kept[row] = (int32_t)number;
+      answer(i, weight(ld_logit(rw.z, i)) / ((double)sum * 0x1p-50), number);
     }
     return;
   }
-  // (a token that is not kept lies at the far end: its weight underflows)
-  auto weight = [&](float x, int i) { return exp2_neg(kept(x, i) ? sc.dist(x) : 1100.0); };
   const int strips = (V + kStrip - 1) / kStrip;
   u64 number = 0;
   double part = 0.0;
@@ -643,14 +758,11 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
       [&](const float (&x)[4], int at) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          double w = weight(x[j], at + j);
           bool in = kept(x[j], at + j);
-          if (min_w > 0.0) {
-            in = in && (w >= min_w || x[j] == sc.zmax);
-            w = in ? w : 0.0;
-          }
+          const double w = exp2_neg(sc.diff(x[j]), sc.c);   // (of no use where it is not kept or too far)
+          if (limit_m) in = in && by_min(x[j], w) && x[j] >= sc.far;
           number += (unsigned)__popcll(__ballot(in));
-          part += w;
+          part += in && x[j] >= sc.far ? w : 0.0;
         }
       },
       [&](int st) {
@@ -691,8 +803,8 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
     four(rw.z, first, V, x);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      w[j] = weight(x[j], first + j);
-      if (!(w[j] >= min_w || x[j] == sc.zmax)) w[j] = 0.0;
+      w[j] = kept(x[j], first + j) ? weight(x[j]) : 0.0;
+      if (!by_min(x[j], w[j])) w[j] = 0.0;
       run += w[j];
     }
     const double inc = wave_scan(run, lane);
@@ -719,11 +831,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
     }
     before += __shfl(inc, kWave - 1);
   }
-  if (lane == 0) {
-    a.tokens[row] = token;
-    if (a.prob) a.prob[row] = (float)(w_token / total);
-    if (a.n_kept) a.n_kept[row] = (int32_t)number;
-  }
+  if (lane == 0) answer(token, w_token / total, number);
 }
 
 // ------------------------------------------------------------------ embedding rows
