@@ -538,6 +538,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
       int b[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) b[j] = sc.bin(x[j], mant[j]);
+      asm volatile("" : "+v"(mant[0]), "+v"(mant[1]), "+v"(mant[2]), "+v"(mant[3]));   // (all four at once)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         if (x[j] >= sc.far_bin) atomicAdd(&s.mass[b[j]], mant[j]);
@@ -598,22 +599,31 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
   // ---- few tokens: each with each
   if (whole && n_list <= kThreads) {
     const bool mine = tid < n_list;
-    const float x = mine ? s.list.z[tid] : 0.f;
-    const int i = mine ? s.list.i[tid] : 0;
+    const float x = mine ? s.list.z[tid] : -INFINITY;   // (the padding comes after everything)
+    const int i = mine ? s.list.i[tid] : 0x7FFFFFFF;
     const double w = mine ? weight(x) : 0.0;
     const u64 un = Scale::units(w);
+    if (!mine) { s.list.z[tid] = x; s.list.i[tid] = i; }
     s.mass[tid] = un;
     __syncthreads();
+    const int n_pad = (n_list + 7) & ~7;
     bool in = mine;
     if (cut_needed) {
       u64 before = 0;
       uint32_t rank = 0;
       if (wave * kWave < n_list) {
-        for (int e = 0; e < n_list; ++e) {
-          const float y = s.list.z[e];
-          const bool first = y > x || (y == x && s.list.i[e] < i);
-          rank += first;
-          before += first ? s.mass[e] : 0;
+        for (int e0 = 0; e0 < n_pad; e0 += 8) {
+          float y[8];
+          int q[8];
+          u64 v[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) { y[e] = s.list.z[e0 + e]; q[e] = s.list.i[e0 + e]; v[e] = s.mass[e0 + e]; }
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const bool first = y[e] > x || (y[e] == x && q[e] < i);
+            rank += first;
+            before += first ? v[e] : 0;
+          }
         }
       }
       if (limit_k) in = in && rank < (uint32_t)k;
@@ -632,7 +642,14 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
     if (target >= sum) target = sum - 1;   // (the last token with a weight)
     if (wave * kWave < n_list) {
       u64 upto = 0;
-      for (int e = 0; e < n_list; ++e) upto += s.list.i[e] <= i ? s.mass[e] : 0;
+      for (int e0 = 0; e0 < n_pad; e0 += 8) {
+        int q[8];
+        u64 v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { q[e] = s.list.i[e0 + e]; v[e] = s.mass[e0 + e]; }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) upto += q[e] <= i ? v[e] : 0;
+      }
       if (in && upto > target) atomicMin(&s.hi, (uint32_t)i);
     }
     __syncthreads();
@@ -756,10 +773,15 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
   __syncthreads();   // (the strips' sums take the list's place)
   rw.strips(
       [&](const float (&x)[4], int at) {
+        // (weights of all four at once, of no use where a token is not kept or too far: a branch around each costs more)
+        double w4[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w4[j] = exp2_neg(sc.diff(x[j]), sc.c);
+        asm volatile("" : "+v"(w4[0]), "+v"(w4[1]), "+v"(w4[2]), "+v"(w4[3]));
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           bool in = kept(x[j], at + j);
-          const double w = exp2_neg(sc.diff(x[j]), sc.c);   // (of no use where it is not kept or too far)
+          const double w = w4[j];
           if (limit_m) in = in && by_min(x[j], w) && x[j] >= sc.far;
           number += (unsigned)__popcll(__ballot(in));
           part += in && x[j] >= sc.far ? w : 0.0;
