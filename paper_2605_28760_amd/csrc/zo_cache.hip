@@ -1,12 +1,14 @@
 // Decoding from a paged key/value cache (Sec. 2.2: a query is a prompt that a candidate continues; the rows of a
 // decode step are one token per sequence, each under its own candidate).
 //
-//   k_cache_append      per-head RMS norm + rotary embedding of new rows, keys and values into their pages
+//   k_cache_append[_heads]  per-head RMS norm + rotary embedding of new rows, keys and values into their pages
 //   k_attention_paged   attention of a new row over its sequence's pages, a range of them per workgroup
 //   k_attention_join    joins the ranges of a long row
 //
 // A row's place: sequence i with cu[i] <= t < cu[i+1], position kv_len[i] - (cu[i+1] - t); position p lies in slot
 // p % page_size of page page_table[i][p / page_size].  Rows behind the last sequence are left as they were.
+#include <math.h>
+
 #include <atomic>
 
 #include "zo_device.hpp"
@@ -49,6 +51,30 @@ __device__ __forceinline__ int page_of(const CacheDev& c, int seq, int pos) {
 // First element of (page, head, slot) in a pool.
 __device__ __forceinline__ int64_t slot_at(const CacheDev& c, int page, int head, int pos) {
   return ((((int64_t)page * c.n_kv_heads + head) << c.page_shift) + (pos & ((1 << c.page_shift) - 1))) * c.dh;
+}
+
+struct Place {
+  int seq, pos;   // seq < 0: behind the last sequence
+};
+
+// Sequence and position of row t, wave-wide: 63 bounds at a time, and the lengths travel with the last of them.
+__device__ __forceinline__ Place place_of_row(const int32_t* cu, const int32_t* kv_len, int S, int t, int lane) {
+  int lo = 0, n = S + 1;   // candidates lo .. lo + n - 1; cu[lo] <= t
+  while (n > 63) {
+    const int step = (n + 62) / 63;
+    const int i = lo + lane * step;
+    const unsigned long long le = __ballot(lane < 63 && lane * step < n && cu[min(i, S)] <= t);
+    const int k = max(__popcll(le) - 1, 0);
+    n = min(step, n - k * step);
+    lo += k * step;
+  }
+  const int i = min(lo + lane, S);
+  const int c = cu[i];
+  const int len = kv_len[min(i, S - 1)];
+  const int k = __popcll(__ballot(lane < n && c <= t)) - 1;
+  if (lo + k >= S) return Place{-1, 0};
+  const int next = __builtin_amdgcn_readlane(c, k + 1);
+  return Place{__builtin_amdgcn_readfirstlane(lo + k), __builtin_amdgcn_readlane(len, k) - (next - t)};
 }
 
 // ------------------------------------------------------------------ append
@@ -120,6 +146,109 @@ __global__ __launch_bounds__(256) void k_cache_append(AppendArgs a) {
   }
 }
 
+// Head dimension 64, 128 or 256, rows aligned: kDh / 8 lanes have a head, each the elements 4 j .. 4 j + 3 and their rotation
+// partners kDh/2 + 4 j .., so that the sum of squares is a few exchanges between neighbours and the rotation stays in the lane.
+// A wave takes rows (one after another where there are many) and `per_wave` groups of 512 / kDh heads of each, the next group's
+// loads under way; angles are formed once per row, frequencies once per wave.  Queries, keys and values are one list of heads.
+// Bound by memory: 17233 rows of 32 + 2 * 8 heads of 128, 96 us (4.4 TB/s;
+// a wave per row and head took 676); 16 rows: the latency of a launch.
+template <typename Tio> struct Four;
+template <> struct Four<bf16_t> {
+  typedef uint2 type;
+  static __device__ __forceinline__ void unpack(const uint2& v, float* x) {
+    x[0] = __uint_as_float(v.x << 16); x[1] = __uint_as_float(v.x & 0xFFFF0000u);
+    x[2] = __uint_as_float(v.y << 16); x[3] = __uint_as_float(v.y & 0xFFFF0000u);
+  }
+  static __device__ __forceinline__ uint2 pack(const float* x) { return make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])); }
+};
+template <> struct Four<float> {
+  typedef float4 type;
+  static __device__ __forceinline__ void unpack(const float4& v, float* x) { x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w; }
+  static __device__ __forceinline__ float4 pack(const float* x) { return make_float4(x[0], x[1], x[2], x[3]); }
+};
+
+template <typename Tio, int kDh>
+__global__ __launch_bounds__(256) void k_cache_append_heads(AppendArgs a, int per_wave, double log2_theta) {
+  typedef Four<Tio> F;
+  typedef typename F::type V4;
+  constexpr int kLanes = kDh / 8, kHeads = kWave / kLanes;   // lanes of a head, heads at a time
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int j = lane % kLanes, hh = lane / kLanes;
+  const int nkv = a.c.n_kv_heads, heads = a.n_heads + 2 * nkv;
+  const int g_first = blockIdx.y * per_wave, g_last = min(g_first + per_wave, (heads + kHeads - 1) / kHeads);
+  double freq[4];   // revolutions per position
+  if (a.theta > 0.f) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) freq[e] = exp2(-(double)(2 * (4 * j + e)) / kDh * log2_theta) * 0.15915494309189533577;
+  }
+  float4 gq0 = make_float4(1.f, 1.f, 1.f, 1.f), gq1 = gq0, gk0 = gq0, gk1 = gq0;
+  if (a.gamma_q) {
+    gq0 = *reinterpret_cast<const float4*>(a.gamma_q + 4 * j);
+    gq1 = *reinterpret_cast<const float4*>(a.gamma_q + kDh / 2 + 4 * j);
+    gk0 = *reinterpret_cast<const float4*>(a.gamma_k + 4 * j);
+    gk1 = *reinterpret_cast<const float4*>(a.gamma_k + kDh / 2 + 4 * j);
+  }
+  for (int t = blockIdx.x * 4 + wave; t < a.T; t += gridDim.x * 4) {
+    auto load = [&](int grp, V4& lo, V4& hi) {
+      const int head = min(grp * kHeads + hh, heads - 1);
+      const Tio* in = head < a.n_heads ? (const Tio*)a.Q + (int64_t)t * a.ldq + head * kDh
+                      : head < a.n_heads + nkv ? (const Tio*)a.K + (int64_t)t * a.ldk + (head - a.n_heads) * kDh
+                                               : (const Tio*)a.V + (int64_t)t * a.ldv + (head - a.n_heads - nkv) * kDh;
+      lo = *reinterpret_cast<const V4*>(in + 4 * j);
+      hi = *reinterpret_cast<const V4*>(in + kDh / 2 + 4 * j);
+    };
+    V4 lo, hi;
+    load(g_first, lo, hi);
+    const Place pl = place_of_row(a.cu, a.c.kv_len, a.S, t, lane);
+    if (pl.seq < 0) continue;
+    const int page = page_of(a.c, pl.seq, pl.pos);
+    float cs[4] = {1.f, 1.f, 1.f, 1.f}, sn[4] = {0.f, 0.f, 0.f, 0.f};
+    if (a.theta > 0.f) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const double turns = (double)pl.pos * freq[e];
+        const float part = (float)(turns - floor(turns));   // (the hardware's sine and cosine take revolutions)
+        cs[e] = __builtin_amdgcn_cosf(part);
+        sn[e] = __builtin_amdgcn_sinf(part);
+      }
+    }
+    for (int grp = g_first; grp < g_last; ++grp) {
+      V4 nlo = lo, nhi = hi;
+      if (grp + 1 < g_last) load(grp + 1, nlo, nhi);
+      const int head = grp * kHeads + hh;
+      const bool is_q = head < a.n_heads, is_v = head >= a.n_heads + nkv;
+      float x[8];   // [0..3] first half, [4..7] partners
+      F::unpack(lo, x);
+      F::unpack(hi, x + 4);
+      if (a.gamma_q) {
+        float ss = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) ss += x[e] * x[e];
+#pragma unroll
+        for (int o = kLanes / 2; o >= 1; o >>= 1) ss += __shfl_xor(ss, o);
+        const float rstd = 1.0f / sqrtf(ss * (1.0f / kDh) + a.eps);
+        const float4 g0 = is_q ? gq0 : gk0, g1 = is_q ? gq1 : gk1;
+        x[0] *= rstd * g0.x; x[1] *= rstd * g0.y; x[2] *= rstd * g0.z; x[3] *= rstd * g0.w;
+        x[4] *= rstd * g1.x; x[5] *= rstd * g1.y; x[6] *= rstd * g1.z; x[7] *= rstd * g1.w;
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float p = x[e], q = x[4 + e];
+        x[e] = p * cs[e] - q * sn[e];
+        x[4 + e] = q * cs[e] + p * sn[e];
+      }
+      if (head < heads && (is_q || page >= 0)) {
+        Tio* out = is_q ? (Tio*)a.Qout + (int64_t)t * a.ldqo + head * kDh
+                        : (Tio*)(is_v ? a.c.V : a.c.K) + slot_at(a.c, page, head - a.n_heads - (is_v ? nkv : 0), pl.pos);
+        *reinterpret_cast<V4*>(out + 4 * j) = is_v ? lo : F::pack(x);
+        *reinterpret_cast<V4*>(out + kDh / 2 + 4 * j) = is_v ? hi : F::pack(x + 4);
+      }
+      lo = nlo;
+      hi = nhi;
+    }
+  }
+}
+
 // ------------------------------------------------------------------ attention
 
 // A row's positions are cut into ranges of range_keys(n), a function of the row's own n alone; two waves take one (row,
@@ -153,30 +282,6 @@ __host__ __device__ constexpr int range_keys(bool bf16, int n) {
 constexpr int most_ranges(bool bf16, int n) {
   const int base = bf16 ? 256 : 128;
   return n >= kMaxRanges * base ? kMaxRanges : (n + base - 1) / base;
-}
-
-struct Place {
-  int seq, pos;   // seq < 0: behind the last sequence
-};
-
-// Sequence and position of row t, wave-wide: 63 bounds at a time, and the lengths travel with the last of them.
-__device__ __forceinline__ Place place_of_row(const int32_t* cu, const int32_t* kv_len, int S, int t, int lane) {
-  int lo = 0, n = S + 1;   // candidates lo .. lo + n - 1; cu[lo] <= t
-  while (n > 63) {
-    const int step = (n + 62) / 63;
-    const int i = lo + lane * step;
-    const unsigned long long le = __ballot(lane < 63 && lane * step < n && cu[min(i, S)] <= t);
-    const int k = max(__popcll(le) - 1, 0);
-    n = min(step, n - k * step);
-    lo += k * step;
-  }
-  const int i = min(lo + lane, S);
-  const int c = cu[i];
-  const int len = kv_len[min(i, S - 1)];
-  const int k = __popcll(__ballot(lane < n && c <= t)) - 1;
-  if (lo + k >= S) return Place{-1, 0};
-  const int next = __builtin_amdgcn_readlane(c, k + 1);
-  return Place{__builtin_amdgcn_readfirstlane(lo + k), __builtin_amdgcn_readlane(len, k) - (next - t)};
 }
 
 // Workspace: [T][n_heads][ranges] of (maximum, sum), then [T][n_heads][ranges][dh] unnormalised outputs.
@@ -601,12 +706,37 @@ __global__ __launch_bounds__(kJoinSums* kWave) void k_attention_join(PagedAttnAr
 
 }  // namespace
 
-hipError_t launch_cache_append(const AppendArgs& a, hipStream_t st) {
-  const int64_t items = (int64_t)a.T * (a.n_heads + 2 * a.c.n_kv_heads);
-  const dim3 grid((unsigned)((items + 3) / 4));
-  if (a.c.bf16) k_cache_append<bf16_t><<<grid, 256, 0, st>>>(a);
-  else k_cache_append<float><<<grid, 256, 0, st>>>(a);
+namespace {
+template <typename Tio, int kDh>
+hipError_t launch_append_heads(const AppendArgs& a, hipStream_t st) {
+  constexpr int kHeads = 512 / kDh;
+  const int groups = (a.n_heads + 2 * a.c.n_kv_heads + kHeads - 1) / kHeads, cus = compute_units();
+  // Few rows: their heads are spread over waves until there are sixteen waves per compute unit.
+  int per_wave = groups;
+  while (per_wave > 1 && (int64_t)a.T * ((groups + per_wave - 1) / per_wave) < 16 * cus) per_wave = (per_wave + 1) / 2;
+  const int splits = (groups + per_wave - 1) / per_wave;
+  const int wgs = (a.T + 3) / 4, most = 8 * cus;   // (one round of waves that stride through the rows)
+  const dim3 grid((unsigned)(wgs < most ? wgs : most), (unsigned)splits);
+  k_cache_append_heads<Tio, kDh><<<grid, 256, 0, st>>>(a, per_wave, a.theta > 0.f ? log2((double)a.theta) : 0.0);
   return hipGetLastError();
+}
+template <typename Tio>
+hipError_t launch_append(const AppendArgs& a, hipStream_t st) {
+  auto aligned = [](const void* p, int64_t ld) { return ((uintptr_t)p & (4 * sizeof(Tio) - 1)) == 0 && ld % 4 == 0; };
+  if (aligned(a.Q, a.ldq) && aligned(a.K, a.ldk) && aligned(a.V, a.ldv) && aligned(a.Qout, a.ldqo) &&
+      (((uintptr_t)a.gamma_q | (uintptr_t)a.gamma_k) & 15u) == 0) {
+    if (a.c.dh == 64) return launch_append_heads<Tio, 64>(a, st);
+    if (a.c.dh == 128) return launch_append_heads<Tio, 128>(a, st);
+    if (a.c.dh == 256) return launch_append_heads<Tio, 256>(a, st);
+  }
+  const int64_t items = (int64_t)a.T * (a.n_heads + 2 * a.c.n_kv_heads);
+  k_cache_append<Tio><<<dim3((unsigned)((items + 3) / 4)), 256, 0, st>>>(a);
+  return hipGetLastError();
+}
+}  // namespace
+
+hipError_t launch_cache_append(const AppendArgs& a, hipStream_t st) {
+  return a.c.bf16 ? launch_append<bf16_t>(a, st) : launch_append<float>(a, st);
 }
 
 int attention_paged_ranges(bool bf16, int max_len) { return max_len > 0 ? most_ranges(bf16, max_len) : 1; }
