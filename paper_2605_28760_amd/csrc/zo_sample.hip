@@ -13,8 +13,8 @@
 //   top-p    a histogram of weights over bins of an eighth of an octave finds the bin in which the prefix ends; inside a bin
 //            the weights' mantissas add up as integers, and their sum tells the number of tokens within 5 %.
 //   min-p    a comparison.
-// Up to kThreads gathered tokens are compared each with each: ranks, weights before them and running sums by index in one
-// sweep.  More of them, up to kList: the bin is cut again by the bits of its logits until one value is left, and equal logits
+// Up to kThreads gathered tokens are ranked by comparing each with each, and their weights summed in that order; the same again
+// by index.  More of them, up to kList: the bin is cut again by the bits of its logits until one value is left, and equal logits
 // are kept by ascending index.  A prefix of more than kList tokens stays in memory: only the last bin's tokens are gathered, and
 // the draw reads the row again for its running sum.
 //
@@ -598,62 +598,71 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
 
   // ---- few tokens: each with each
   if (whole && n_list <= kThreads) {
-    const bool mine = tid < n_list;
-    const float x = mine ? s.list.z[tid] : -INFINITY;   // (the padding comes after everything)
-    const int i = mine ? s.list.i[tid] : 0x7FFFFFFF;
-    const double w = mine ? weight(x) : 0.0;
-    const u64 un = Scale::units(w);
-    if (!mine) { s.list.z[tid] = x; s.list.i[tid] = i; }
-    s.mass[tid] = un;
-    __syncthreads();
-    const int n_pad = (n_list + 7) & ~7;
-    bool in = mine;
-    if (cut_needed) {
-      u64 before = 0;
-      uint32_t rank = 0;
-      if (wave * kWave < n_list) {
-        for (int e0 = 0; e0 < n_pad; e0 += 8) {
-          float y[8];
-          int q[8];
-          u64 v[8];
+    u64* const keys = reinterpret_cast<u64*>(&s.list.z[kList / 2]);   // (behind the tokens)
+    float* const lz = s.list.z;
+    int32_t* const li = s.list.i;
+    // How many of the n keys are larger than thread tid's: s.cnt[tid].  Where there are fewer keys than threads, several threads
+    // share one's comparisons.
+    auto ranks = [&](u64 key, int n) __attribute__((always_inline)) {
+      int width = kWave;
+      while (width < n) width <<= 1;
+      keys[tid] = key;   // (0 behind the n-th)
+      s.cnt[tid] = 0;
+      __syncthreads();
+      const int mine = tid & (width - 1), share = (n * (width / kWave) + kThreads / kWave * 8 - 1) / (kThreads / kWave * 8) * 8;
+      const int from = tid / width * share, upto = min(from + share, (n + 7) & ~7);
+      const u64 own = keys[mine];
+      uint32_t r = 0;
+      for (int e0 = from; e0 < upto; e0 += 8) {
+        u64 y[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) { y[e] = s.list.z[e0 + e]; q[e] = s.list.i[e0 + e]; v[e] = s.mass[e0 + e]; }
+        for (int e = 0; e < 8; ++e) y[e] = keys[e0 + e];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const bool first = y[e] > x || (y[e] == x && q[e] < i);
-            rank += first;
-            before += first ? v[e] : 0;
-          }
-        }
+        for (int e = 0; e < 8; ++e) r += y[e] > own;
       }
-      if (limit_k) in = in && rank < (uint32_t)k;
-      if (limit_p) {
-        const double z_k = limit_k ? (double)block_sum(s, lane, wave, in ? un : 0) * 0x1p-50 : z_all;
-        in = in && (rank == 0 || (double)before * 0x1p-50 < (double)p * z_k);
-      }
+      if (r) atomicAdd(&s.cnt[mine], r);
+      __syncthreads();
+    };
+    int n = n_list;
+    float x = tid < n ? lz[tid] : -INFINITY;
+    int i = tid < n ? li[tid] : 0;
+    u64 nb;
+    double mb;
+    if (cut_needed) {   // in order, as far as top-k goes
+      ranks(tid < n ? (u64)key_of(x) << 32 | (uint32_t)~i : 0, n);
+      const int rank = s.cnt[tid];
+      if (tid < n) { lz[rank] = x; li[rank] = i; }
+      __syncthreads();
+      if (limit_k && n > k) n = k;
+      x = tid < n ? lz[tid] : -INFINITY;
+      i = tid < n ? li[tid] : 0;
+    }
+    bool in = tid < n;
+    const double w = in ? weight(x) : 0.0;
+    u64 un = Scale::units(w);
+    if (limit_p) {
+      const double z_k = limit_k ? (double)block_sum(s, lane, wave, un) * 0x1p-50 : z_all;
+      block_scan(s, lane, wave, un, 0.0, nb, mb);
+      in = in && (tid == 0 || (double)nb * 0x1p-50 < (double)p * z_k);
     }
     in = in && by_min(x, w);
-    const u64 sum = block_sum(s, lane, wave, in ? un : 0);
+    un = in ? un : 0;
+    const u64 sum = block_sum(s, lane, wave, un);
     const u64 number = block_sum(s, lane, wave, (u64)in);
-    s.mass[tid] = in ? un : 0;
-    if (tid == 0) s.hi = 0x7FFFFFFFu;
-    __syncthreads();
     u64 target = (u64)(u1 * (double)sum);
     if (target >= sum) target = sum - 1;   // (the last token with a weight)
-    if (wave * kWave < n_list) {
-      u64 upto = 0;
-      for (int e0 = 0; e0 < n_pad; e0 += 8) {
-        int q[8];
-        u64 v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) { q[e] = s.list.i[e0 + e]; v[e] = s.mass[e0 + e]; }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) upto += q[e] <= i ? v[e] : 0;
-      }
-      if (in && upto > target) atomicMin(&s.hi, (uint32_t)i);
-    }
+    // by index: their running sum
     __syncthreads();
-    if (in && (uint32_t)i == s.hi) answer(i, w / ((double)sum * 0x1p-50), number);
+    ranks(in ? (u64)(uint32_t)~i : 0, n);
+    s.mass[tid] = 0;
+    __syncthreads();
+    const int place = s.cnt[tid];
+    if (in) s.mass[place] = un;
+    __syncthreads();
+    block_scan(s, lane, wave, s.mass[tid], 0.0, nb, mb);
+    if (nb <= target && nb + s.mass[tid] > target) s.bin = tid;
+    __syncthreads();
+    if (in && place == s.bin) answer(i, w / ((double)sum * 0x1p-50), number);
     return;
   }
 
