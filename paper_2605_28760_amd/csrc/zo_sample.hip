@@ -19,6 +19,8 @@
 // the draw reads the row again for its running sum.
 //
 // One workgroup of 16 waves per row; what bounds it is the double-precision arithmetic, 20 operations for a weight.
+#include <atomic>
+
 #include "zo_device.hpp"
 #include "zo_internal.hpp"
 
@@ -164,6 +166,7 @@ struct Shared {
     struct { float z[kList]; int32_t i[kList]; } list;
     double strip[kMaxStrips];
   };
+  float packed[kWaves][kStrip / 2];
   u64 wave_n[kWaves];
   double wave_m[kWaves];
   float wave_z[kWaves];
@@ -214,6 +217,23 @@ struct Row {
   template <class F>
   __device__ __forceinline__ void strips(F f) const {
     strips(f, [](int) {});
+  }
+  // f(x, first index, strip) for the lane's 4 * kPieces tokens of a strip at once
+  template <class F>
+  __device__ __forceinline__ void whole_strips(F f) const {
+    float x[kPieces][4];
+    int u = 0, first = 0;
+    strips(
+        [&](const float (&y)[4], int at) {
+          if (u == 0) first = at;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[u & (kPieces - 1)][j] = y[j];
+          ++u;
+        },
+        [&](int st) {
+          f(x, first, st);
+          u = 0;
+        });
   }
 };
 
@@ -596,47 +616,49 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
   }
   int n_list = whole ? (int)s.n_list : 0;
 
-  // ---- few tokens: each with each
+  // ---- short lists: each with each
+  u64* const keys = reinterpret_cast<u64*>(&s.list.z[kList / 2]);   // (behind kThreads tokens)
+  float* const lz = s.list.z;
+  int32_t* const li = s.list.i;
+  // How many of the n <= kThreads keys are larger than thread tid's: s.cnt[tid].  Where there are fewer keys than threads,
+  // several threads share one's comparisons.
+  auto ranks = [&](u64 key, int n) __attribute__((always_inline)) {
+    int width = kWave;
+    while (width < n) width <<= 1;
+    keys[tid] = key;   // (0 behind the n-th)
+    s.cnt[tid] = 0;
+    __syncthreads();
+    const int mine = tid & (width - 1), share = (n * (width / kWave) + kThreads / kWave * 8 - 1) / (kThreads / kWave * 8) * 8;
+    const int from = tid / width * share, upto = min(from + share, (n + 7) & ~7);
+    const u64 own = keys[mine];
+    uint32_t r = 0;
+    for (int e0 = from; e0 < upto; e0 += 8) {
+      u64 y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = keys[e0 + e];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) r += y[e] > own;
+    }
+    if (r) atomicAdd(&s.cnt[mine], r);
+    __syncthreads();
+  };
+  // the first n <= kThreads tokens of the list in order
+  auto sort_list = [&](int n) __attribute__((always_inline)) {
+    const float x = tid < n ? lz[tid] : -INFINITY;
+    const int i = tid < n ? li[tid] : 0;
+    ranks(tid < n ? (u64)key_of(x) << 32 | (uint32_t)~i : 0, n);
+    const int rank = s.cnt[tid];
+    if (tid < n) { lz[rank] = x; li[rank] = i; }
+    __syncthreads();
+  };
   if (whole && n_list <= kThreads) {
-    u64* const keys = reinterpret_cast<u64*>(&s.list.z[kList / 2]);   // (behind the tokens)
-    float* const lz = s.list.z;
-    int32_t* const li = s.list.i;
-    // How many of the n keys are larger than thread tid's: s.cnt[tid].  Where there are fewer keys than threads, several threads
-    // share one's comparisons.
-    auto ranks = [&](u64 key, int n) __attribute__((always_inline)) {
-      int width = kWave;
-      while (width < n) width <<= 1;
-      keys[tid] = key;   // (0 behind the n-th)
-      s.cnt[tid] = 0;
-      __syncthreads();
-      const int mine = tid & (width - 1), share = (n * (width / kWave) + kThreads / kWave * 8 - 1) / (kThreads / kWave * 8) * 8;
-      const int from = tid / width * share, upto = min(from + share, (n + 7) & ~7);
-      const u64 own = keys[mine];
-      uint32_t r = 0;
-      for (int e0 = from; e0 < upto; e0 += 8) {
-        u64 y[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = keys[e0 + e];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) r += y[e] > own;
-      }
-      if (r) atomicAdd(&s.cnt[mine], r);
-      __syncthreads();
-    };
     int n = n_list;
-    float x = tid < n ? lz[tid] : -INFINITY;
-    int i = tid < n ? li[tid] : 0;
     u64 nb;
     double mb;
-    if (cut_needed) {   // in order, as far as top-k goes
-      ranks(tid < n ? (u64)key_of(x) << 32 | (uint32_t)~i : 0, n);
-      const int rank = s.cnt[tid];
-      if (tid < n) { lz[rank] = x; li[rank] = i; }
-      __syncthreads();
-      if (limit_k && n > k) n = k;
-      x = tid < n ? lz[tid] : -INFINITY;
-      i = tid < n ? li[tid] : 0;
-    }
+    if (cut_needed) sort_list(n);
+    if (limit_k && n > k) n = k;
+    const float x = tid < n ? lz[tid] : -INFINITY;
+    const int i = tid < n ? li[tid] : 0;
     bool in = tid < n;
     const double w = in ? weight(x) : 0.0;
     u64 un = Scale::units(w);
@@ -730,15 +752,32 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
       gather(bin_p, bin_p);
       n_list = s.n_list <= kList ? (int)s.n_list : 0;
     }
-    // (what the counts before the bin are does not matter)
-    if (whole || n_list > 0) refine(s, sc, tid, lane, wave, bin_p, 0, m_to, by_mass, each_listed);
+    if (!whole && n_list > 0 && n_list <= kThreads) {
+      sort_list(n_list);
+      const bool in = tid < n_list;
+      const float x = in ? lz[tid] : -INFINITY;
+      const u64 un = in ? Scale::units(weight(x)) : 0;
+      u64 nb;
+      double mb;
+      block_scan(s, lane, wave, un, 0.0, nb, mb);
+      // (the bin was chosen because the limit lies in it: its first token is kept)
+      if (tid == 0) s.index = 0;
+      __syncthreads();
+      if (in && m_to + (double)nb * 0x1p-50 < by_mass.mass) atomicMax(&s.index, tid);
+      __syncthreads();
+      cut.key = key_of(lz[s.index]);
+      cut.limit = li[s.index];
+      ties = 0;   // (settled)
+    } else if (whole || n_list > 0) refine(s, sc, tid, lane, wave, bin_p, 0, m_to, by_mass, each_listed);
     else refine(s, sc, tid, lane, wave, bin_p, 0, m_to, by_mass, each_token);
-    cut.key = s.lo;
-    ties = s.n_at;
+    if (whole || n_list == 0 || n_list > kThreads) {
+      cut.key = s.lo;
+      ties = s.n_at;
+    }
   }
   __syncthreads();
   // ---- equal logits at the cut are kept by ascending index
-  if (cut_needed) {
+  if (cut_needed && ties > 0) {
     if (whole || (!limit_k && n_list > 0))
       list_index(s, tid, lane, wave, n_list, V, ties - 1, [&](float x, int) { return (u64)(key_of(x) == cut.key); });
     else
@@ -778,29 +817,50 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
   }
   const int strips = (V + kStrip - 1) / kStrip;
   u64 number = 0;
-  double part = 0.0;
   __syncthreads();   // (the strips' sums take the list's place)
-  rw.strips(
-      [&](const float (&x)[4], int at) {
-        // (weights of all four at once, of no use where a token is not kept or too far: a branch around each costs more)
-        double w4[4];
+  float* const packed = s.packed[wave];
+  rw.whole_strips([&](const float (&x)[kPieces][4], int first, int st) {
+    u64 in[kPieces][4];
+    int n = 0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) w4[j] = exp2_neg(sc.diff(x[j]), sc.c);
-        asm volatile("" : "+v"(w4[0]), "+v"(w4[1]), "+v"(w4[2]), "+v"(w4[3]));
+    for (int u = 0; u < kPieces; ++u)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        in[u][j] = __ballot(kept(x[u][j], first + u * (4 * kWave) + j));
+        n += __popcll(in[u][j]);
+      }
+    double part = 0.0;
+    auto add = [&](float z, bool there) __attribute__((always_inline)) {
+      double w = exp2_neg(sc.diff(z), sc.c);   // (of no use where there is none, or too far)
+      asm volatile("" : "+v"(w));
+      bool take = there && z >= sc.far;
+      if (limit_m) {
+        take = take && by_min(z, w);
+        number += (unsigned)__popcll(__ballot(take));
+      }
+      part += take ? w : 0.0;
+    };
+    if (!limit_m) number += (unsigned)n;
+    if (n > kStrip / 2) {
+#pragma unroll
+      for (int u = 0; u < kPieces; ++u)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) add(x[u][j], in[u][j] >> lane & 1);
+    } else {   // the kept ones packed: an exponential costs more than moving them
+      int at = 0;
+#pragma unroll
+      for (int u = 0; u < kPieces; ++u)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          bool in = kept(x[j], at + j);
-          const double w = w4[j];
-          if (limit_m) in = in && by_min(x[j], w) && x[j] >= sc.far;
-          number += (unsigned)__popcll(__ballot(in));
-          part += in && x[j] >= sc.far ? w : 0.0;
+          const u64 m = in[u][j];
+          if (m >> lane & 1) packed[at + __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0))] = x[u][j];
+          at += __popcll(m);
         }
-      },
-      [&](int st) {
-        const double sum = wave_sum(part);
-        if (lane == 0) s.strip[st] = sum;
-        part = 0.0;
-      });
+      for (int e = 0; e < n; e += kWave) add(e + lane < n ? packed[e + lane] : 0.f, e + lane < n);
+    }
+    const double sum = wave_sum(part);
+    if (lane == 0) s.strip[st] = sum;
+  });
   if (lane == 0) s.wave_n[wave] = number;
   __syncthreads();
   number = 0;
@@ -932,10 +992,21 @@ __global__ __launch_bounds__(256) void k_embed_rows(EmbedArgs a) {
 
 }  // namespace
 
-hipError_t launch_sample(const SampleArgs& a, hipStream_t st) {
-  if (a.bf16) k_sample<bf16_t><<<dim3(a.T), kThreads, sizeof(Shared), st>>>(a);
-  else k_sample<float><<<dim3(a.T), kThreads, sizeof(Shared), st>>>(a);
+namespace {
+template <typename Tio>
+hipError_t launch_sample_of(const SampleArgs& a, hipStream_t st) {
+  static std::atomic<bool> ready[kMaxDevices];
+  const hipError_t e = once_per_device(ready, [] {
+    return hipFuncSetAttribute((const void*)k_sample<Tio>, hipFuncAttributeMaxDynamicSharedMemorySize, sizeof(Shared));
+  });
+  if (e != hipSuccess) return e;
+  k_sample<Tio><<<dim3(a.T), kThreads, sizeof(Shared), st>>>(a);
   return hipGetLastError();
+}
+}  // namespace
+
+hipError_t launch_sample(const SampleArgs& a, hipStream_t st) {
+  return a.bf16 ? launch_sample_of<bf16_t>(a, st) : launch_sample_of<float>(a, st);
 }
 
 hipError_t launch_embed_rows(const EmbedArgs& a, hipStream_t st) {
