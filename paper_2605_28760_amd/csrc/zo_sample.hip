@@ -13,7 +13,7 @@
 //   top-p    a histogram of weights over bins of an eighth of an octave finds the bin in which the prefix ends; inside a bin
 //            the weights' mantissas add up as integers, and their sum tells the number of tokens within 5 %.
 //   min-p    a comparison.
-// Up to kThreads gathered tokens are ranked by comparing each with each, and their weights summed in that order; the same again
+// Up to kShort gathered tokens are ranked by comparing each with each, and their weights summed in that order; the same again
 // by index.  More of them, up to kList: the bin is cut again by the bits of its logits until one value is left, and equal logits
 // are kept by ascending index.  A prefix of more than kList tokens stays in memory: only the last bin's tokens are gathered, and
 // the draw reads the row again for its running sum.
@@ -36,6 +36,7 @@ constexpr int kStrip = kPieces * 4 * kWave;
 constexpr int kMaxVocab = 1 << 19;
 constexpr int kMaxStrips = kMaxVocab / kStrip;
 constexpr int kList = 4096;          // tokens that fit in LDS
+constexpr int kShort = 512;          // tokens that are ranked by comparing each with each (7 us; 1024 take 27, cutting a bin 18)
 
 typedef unsigned long long u64;
 
@@ -143,21 +144,32 @@ struct Scale {
 };
 __device__ __forceinline__ double bin_unit(int bin) { return bin >= kLast ? 0.0 : exp2_neg((double)bin, 0.125) * 0x1p-44; }
 
+// A lane's value moved by DPP, zero where none arrives: the steps of a running sum over the wave (shifts by 1, 2, 4, 8 within rows
+// of 16 lanes, then the rows' last values).
+template <int kCtrl, int kRows>
+__device__ __forceinline__ uint32_t moved(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kCtrl, kRows, 0xf, false); }
+template <int kCtrl, int kRows>
+__device__ __forceinline__ int moved(int v) { return (int)moved<kCtrl, kRows>((uint32_t)v); }
+template <int kCtrl, int kRows>
+__device__ __forceinline__ u64 moved(u64 v) {
+  return (u64)moved<kCtrl, kRows>((uint32_t)(v >> 32)) << 32 | moved<kCtrl, kRows>((uint32_t)v);
+}
+template <int kCtrl, int kRows>
+__device__ __forceinline__ double moved(double v) { return __longlong_as_double((long long)moved<kCtrl, kRows>((u64)__double_as_longlong(v))); }
 template <class T>
-__device__ __forceinline__ T wave_sum(T v) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o);
+__device__ __forceinline__ T wave_scan(T v) {   // inclusive
+  v += moved<0x111, 0xf>(v);
+  v += moved<0x112, 0xf>(v);
+  v += moved<0x114, 0xf>(v);
+  v += moved<0x118, 0xf>(v);
+  v += moved<0x142, 0xa>(v);
+  v += moved<0x143, 0xc>(v);
   return v;
 }
 template <class T>
-__device__ __forceinline__ T wave_scan(T v, int lane) {   // inclusive
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const T x = __shfl_up(v, o);
-    if (lane >= o) v += x;
-  }
-  return v;
-}
+__device__ __forceinline__ T of_lane(T v, int lane) { return __shfl(v, lane); }
+template <class T>
+__device__ __forceinline__ T wave_sum(T v) { return of_lane(wave_scan(v), kWave - 1); }
 
 struct Shared {
   uint32_t cnt[kBins];
@@ -240,8 +252,8 @@ struct Row {
 // Inclusive running sums over the threads of the workgroup, in a fixed order.  `before` is the sum of the threads before.
 // (Begins and ends with a barrier: the buffers may be in use on either side.)
 __device__ __forceinline__ void block_scan(Shared& s, int lane, int wave, u64 n, double m, u64& n_before, double& m_before) {
-  const u64 ni = wave_scan(n, lane);
-  const double mi = wave_scan(m, lane);
+  const u64 ni = wave_scan(n);
+  const double mi = wave_scan(m);
   __syncthreads();
   if (lane == kWave - 1) { s.wave_n[wave] = ni; s.wave_m[wave] = mi; }
   __syncthreads();
@@ -422,12 +434,12 @@ __device__ __forceinline__ void nth_index(const Row<Tio>& rw, u64 n, Is is) {
       int here = 0;
 #pragma unroll
       for (int j = 0; j < 4; ++j) here += is(x[j]);
-      const int inc = wave_scan(here, rw.lane);
+      const int inc = wave_scan(here);
       u64 b = seen + (u64)(inc - here);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         if (is(x[j]) && b++ == n) s.index = at + j;
-      seen += (u64)__shfl(inc, kWave - 1);
+      seen += (u64)of_lane(inc, kWave - 1);
     }
   }
   __syncthreads();
@@ -620,7 +632,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
   u64* const keys = reinterpret_cast<u64*>(&s.list.z[kList / 2]);   // (behind kThreads tokens)
   float* const lz = s.list.z;
   int32_t* const li = s.list.i;
-  // How many of the n <= kThreads keys are larger than thread tid's: s.cnt[tid].  Where there are fewer keys than threads,
+  // How many of the n <= kShort keys are larger than thread tid's: s.cnt[tid].  Where there are fewer keys than threads,
   // several threads share one's comparisons.
   auto ranks = [&](u64 key, int n) __attribute__((always_inline)) {
     int width = kWave;
@@ -642,7 +654,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
     if (r) atomicAdd(&s.cnt[mine], r);
     __syncthreads();
   };
-  // the first n <= kThreads tokens of the list in order
+  // the n <= kShort tokens of the list in order
   auto sort_list = [&](int n) __attribute__((always_inline)) {
     const float x = tid < n ? lz[tid] : -INFINITY;
     const int i = tid < n ? li[tid] : 0;
@@ -651,7 +663,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
     if (tid < n) { lz[rank] = x; li[rank] = i; }
     __syncthreads();
   };
-  if (whole && n_list <= kThreads) {
+  if (whole && n_list <= kShort) {
     int n = n_list;
     u64 nb;
     double mb;
@@ -752,7 +764,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
       gather(bin_p, bin_p);
       n_list = s.n_list <= kList ? (int)s.n_list : 0;
     }
-    if (!whole && n_list > 0 && n_list <= kThreads) {
+    if (!whole && n_list > 0 && n_list <= kShort) {
       sort_list(n_list);
       const bool in = tid < n_list;
       const float x = in ? lz[tid] : -INFINITY;
@@ -770,7 +782,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
       ties = 0;   // (settled)
     } else if (whole || n_list > 0) refine(s, sc, tid, lane, wave, bin_p, 0, m_to, by_mass, each_listed);
     else refine(s, sc, tid, lane, wave, bin_p, 0, m_to, by_mass, each_token);
-    if (whole || n_list == 0 || n_list > kThreads) {
+    if (whole || n_list == 0 || n_list > kShort) {
       cut.key = s.lo;
       ties = s.n_at;
     }
@@ -820,15 +832,25 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
   __syncthreads();   // (the strips' sums take the list's place)
   float* const packed = s.packed[wave];
   rw.whole_strips([&](const float (&x)[kPieces][4], int first, int st) {
-    u64 in[kPieces][4];
-    int n = 0;
+    bool in[kPieces][4], equal = false;
 #pragma unroll
     for (int u = 0; u < kPieces; ++u)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        in[u][j] = __ballot(kept(x[u][j], first + u * (4 * kWave) + j));
-        n += __popcll(in[u][j]);
+        in[u][j] = x[u][j] >= z_cut;   // (false for NaN)
+        equal = equal || x[u][j] == z_cut;
       }
+    if (__any(equal)) {   // (equal logits at the cut: as far as the limit)
+#pragma unroll
+      for (int u = 0; u < kPieces; ++u)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) in[u][j] = kept(x[u][j], first + u * (4 * kWave) + j);
+    }
+    int n = 0;
+#pragma unroll
+    for (int u = 0; u < kPieces; ++u)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) n += __popcll(__ballot(in[u][j]));
     double part = 0.0;
     auto add = [&](float z, bool there) __attribute__((always_inline)) {
       double w = exp2_neg(sc.diff(z), sc.c);   // (of no use where there is none, or too far)
@@ -845,15 +867,15 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
 #pragma unroll
       for (int u = 0; u < kPieces; ++u)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) add(x[u][j], in[u][j] >> lane & 1);
+        for (int j = 0; j < 4; ++j) add(x[u][j], in[u][j]);
     } else {   // the kept ones packed: an exponential costs more than moving them
       int at = 0;
 #pragma unroll
       for (int u = 0; u < kPieces; ++u)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const u64 m = in[u][j];
-          if (m >> lane & 1) packed[at + __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0))] = x[u][j];
+          const u64 m = __ballot(in[u][j]);
+          if (in[u][j]) packed[at + __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0))] = x[u][j];
           at += __popcll(m);
         }
       for (int e = 0; e < n; e += kWave) add(e + lane < n ? packed[e + lane] : 0.f, e + lane < n);
@@ -898,7 +920,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
       if (!by_min(x[j], w[j])) w[j] = 0.0;
       run += w[j];
     }
-    const double inc = wave_scan(run, lane);
+    const double inc = wave_scan(run);
     double b = before + (inc - run);
     int mine = -1, last = -1;
     double w_mine = 0.0, w_last = 0.0;
@@ -920,7 +942,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
       w_token = __shfl(wi, src);
       if (pass) break;
     }
-    before += __shfl(inc, kWave - 1);
+    before += of_lane(inc, kWave - 1);
   }
   if (lane == 0) answer(token, w_token / total, number);
 }
