@@ -198,16 +198,23 @@ struct Row {
   bool vec;
 
   // f(x, first index) for every four tokens of a strip of kStrip tokens, strip by strip of this wave's share, then
-  // done(strip).  A whole strip's loads are under way together; they are not conditional, or the next would wait for the last.
+  // done(strip).  A whole strip's loads are under way together, and those of the next one under its work.
   template <class F, class Done>
   __device__ __forceinline__ void strips(F f, Done done) const {
     const int n = (V + kStrip - 1) / kStrip, whole = vec ? V / kStrip : 0;
     typedef typename Raw<Tio>::type R;
     int st = wave;
+    R next[kPieces];
+    auto load = [&](int at) __attribute__((always_inline)) {
+#pragma unroll
+      for (int u = 0; u < kPieces; ++u) next[u] = *reinterpret_cast<const R*>(z + at * kStrip + u * (4 * kWave) + lane * 4);
+    };
+    if (st < whole) load(st);
     for (; st < whole; st += kWaves) {
       R raw[kPieces];
 #pragma unroll
-      for (int u = 0; u < kPieces; ++u) raw[u] = *reinterpret_cast<const R*>(z + st * kStrip + u * (4 * kWave) + lane * 4);
+      for (int u = 0; u < kPieces; ++u) raw[u] = next[u];
+      load(min(st + kWaves, whole - 1));   // (not conditional; the last one is loaded again)
 #pragma unroll
       for (int u = 0; u < kPieces; ++u) {
         float x[4];
@@ -609,7 +616,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
     __syncthreads();
     if (tid == 0) s.n_list = 0;
     __syncthreads();
-    rw.strips([&](const float (&x)[4], int at) {
+    rw.strips([&](const float (&x)[4], int at) {   // (tokens that come in are rare: a branch each)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         if (!(x[j] >= least)) continue;
@@ -852,9 +859,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) n += __popcll(__ballot(in[u][j]));
     double part = 0.0;
-    auto add = [&](float z, bool there) __attribute__((always_inline)) {
-      double w = exp2_neg(sc.diff(z), sc.c);   // (of no use where there is none, or too far)
-      asm volatile("" : "+v"(w));
+    auto add = [&](float z, bool there, double w) __attribute__((always_inline)) {
       bool take = there && z >= sc.far;
       if (limit_m) {
         take = take && by_min(z, w);
@@ -866,8 +871,15 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
     if (n > kStrip / 2) {
 #pragma unroll
       for (int u = 0; u < kPieces; ++u)
+        {
+          // (four at once, of no use where a token is not kept or too far: a branch around each costs more)
+          double w[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) add(x[u][j], in[u][j]);
+          for (int c = 0; c < 4; ++c) w[c] = exp2_neg(sc.diff(x[u][c]), sc.c);
+          asm volatile("" : "+v"(w[0]), "+v"(w[1]), "+v"(w[2]), "+v"(w[3]));
+#pragma unroll
+          for (int c = 0; c < 4; ++c) add(x[u][c], in[u][c], w[c]);
+        }
     } else {   // the kept ones packed: an exponential costs more than moving them
       int at = 0;
 #pragma unroll
@@ -878,7 +890,10 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
           if (in[u][j]) packed[at + __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0))] = x[u][j];
           at += __popcll(m);
         }
-      for (int e = 0; e < n; e += kWave) add(e + lane < n ? packed[e + lane] : 0.f, e + lane < n);
+      for (int e = 0; e < n; e += kWave) {
+        const float z = e + lane < n ? packed[e + lane] : sc.zmax;
+        add(z, e + lane < n, exp2_neg(sc.diff(z), sc.c));
+      }
     }
     const double sum = wave_sum(part);
     if (lane == 0) s.strip[st] = sum;
