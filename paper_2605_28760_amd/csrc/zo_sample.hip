@@ -316,19 +316,9 @@ struct Cut {
 template <class Each>
 __device__ __forceinline__ void refine(Shared& s, const Scale& sc, int tid, int lane, int wave, int bin, u64 n0, double m0, const Goal& goal, Each each) {
   const double unit = bin_unit(bin);
-  __syncthreads();
-  if (tid == 0) { s.lo = 0xFFFFFFFFu; s.hi = 0; }
-  __syncthreads();
-  uint32_t klo = 0xFFFFFFFFu, khi = 0;
-  each([&](float x, int) {
-    if (sc.bin(x) != bin) return;
-    klo = min(klo, key_of(x));
-    khi = max(khi, key_of(x));
-  });
-  atomicMin(&s.lo, klo);
-  atomicMax(&s.hi, khi);
-  __syncthreads();
-  uint32_t lo = s.lo, hi = s.hi;
+  // (the logits between the middles of the bins on either side; which of them are the bin's is looked at token by token)
+  float z_lo = bin >= kLast ? kLeast : sc.below((bin + 1) * 0.125, false), z_hi = bin == 0 ? sc.zmax : sc.below((bin - 1) * 0.125, true);
+  uint32_t lo = key_of(z_lo), hi = key_of(z_hi);
   for (;;) {   // (a round leaves at most a 512th of the keys: four rounds)
     int shift = 0;
     while (((hi - lo) >> shift) >= (uint32_t)kBins) ++shift;
@@ -337,9 +327,8 @@ __device__ __forceinline__ void refine(Shared& s, const Scale& sc, int tid, int 
     s.mass[tid] = 0;
     __syncthreads();
     each([&](float x, int) {
-      const uint32_t key = key_of(x);
-      if (key < lo || key > hi || sc.bin(x) != bin) return;
-      const int b = (int)((hi - key) >> shift);
+      if (!(x >= z_lo && x <= z_hi) || sc.bin(x) != bin) return;
+      const int b = (int)((hi - key_of(x)) >> shift);
       atomicAdd(&s.cnt[b], 1u);
       if (bin < kLast) {
         u64 mant;
@@ -372,6 +361,8 @@ __device__ __forceinline__ void refine(Shared& s, const Scale& sc, int tid, int 
     const uint32_t width = (1u << shift) - 1;
     lo = top - lo > width ? top - width : lo;
     hi = top;
+    z_lo = of_key(lo);
+    z_hi = of_key(hi);
   }
 }
 
