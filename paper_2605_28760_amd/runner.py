@@ -4,8 +4,12 @@ and sequences the C-ABI calls of one step:
 
     zo_probe_linear (per layer) -> zo_score -> zo_estimate -> zo_bank_update
 
+and those of an answer (DecodeDriver).
+
 Nothing is computed here; every number comes out of libzo.so.
 """
+import copy
+
 import numpy as np
 import torch
 
@@ -255,6 +259,162 @@ class DeviceModel:
         self.graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(self.graph):
             self.step(lr, update, stream=torch.cuda.current_stream())
+        return self.graph
+
+    def replay(self):
+        self.graph.replay()
+
+
+class DeviceCache:
+    """Key/value caches of n_layers layers for n_seqs sequences of up to max_len positions each: pools of pages, one page
+    table and one length per sequence for all layers, and a zo_cache per layer.  Without a table of the caller's
+    every sequence has pages of its own, in order."""
+
+    def __init__(self, n_layers, n_seqs, max_len, n_kv_heads, head_dim, dtype, device, page_size=64, table=None, n_pages=None):
+        self.max_pages = max(-(-int(max_len) // page_size), 1)
+        if table is None:
+            table = np.arange(n_seqs * self.max_pages, dtype=np.int32).reshape(n_seqs, self.max_pages)
+        self.n_pages = int(n_pages if n_pages is not None else table.max() + 1 if table.size else 1)
+        self.table = torch.from_numpy(np.ascontiguousarray(table, np.int32)).to(device)
+        self.max_pages, self.max_len = int(self.table.shape[1]), int(self.table.shape[1]) * page_size
+        self.kv_len = torch.zeros(n_seqs, device=device, dtype=torch.int32)
+        shape = (max(self.n_pages, 1), n_kv_heads, page_size, head_dim)
+        self.K = [torch.empty(shape, device=device, dtype=_tt(dtype)) for _ in range(n_layers)]
+        self.V = [torch.empty(shape, device=device, dtype=_tt(dtype)) for _ in range(n_layers)]
+        self.structs = [zb.make_cache(k, v, _dt(dtype), self.table, self.kv_len) for k, v in zip(self.K, self.V)]
+
+
+class CachedBlock(DeviceBlock):
+    """A DeviceBlock whose keys and values live in a cache: its rows continue their sequences there.  With `prompt` the rows
+    are whole prompts that enter an empty cache, and attention runs on the packed rows themselves."""
+
+    def __init__(self, d, blk, base, cache, prompt):
+        super().__init__(d, blk, base)
+        self.cache, self.prompt = cache, prompt
+        b = self.blk
+        self.q = torch.empty_like(self.att)
+        self.ws_bytes = 0 if prompt else zb.zo_attention_paged_workspace_bytes(
+            d.batch.T, b.n_heads, b.head_dim, cache.max_pages * cache.page_size, _dt(d.dtype))
+        self.ws = torch.empty(max(self.ws_bytes, 256), device=d.device, dtype=torch.uint8)
+
+    def qk_norm_rope(self, qkv, stream=None, batch=None):
+        if self.prompt:   # (a prompt's positions are its rows' offsets)
+            super().qk_norm_rope(qkv, stream, batch)
+
+    def attention(self, qkv, out, stream=None, batch=None):
+        b, d = self.blk, self.d
+        batch = batch or d.batch
+        nq, nkv, ld = b.n_heads * b.head_dim, b.n_kv_heads * b.head_dim, qkv.stride(0)
+        gq, gk, theta = (None, None, 0.0) if self.prompt else (self.gq, self.gk, float(self.rope_theta or 0.0))
+        zb.zo_cache_append(batch.struct, qkv, ld, qkv[:, nq:], ld, qkv[:, nq + nkv:], ld, b.n_heads, gq, gk,
+                           float(b.norm_eps), theta, self.cache, self.q, nq, stream)
+        if self.prompt:
+            super().attention(qkv, out, stream, batch)
+        else:
+            zb.zo_attention_paged(batch.struct, self.q, nq, b.n_heads, float(b.scale), self.cache, out, out.stride(0),
+                                  self.ws, self.ws_bytes, stream)
+
+
+class DecodeDriver:
+    """Answers of a whole model (workloads.decoder_model) to the prompts of its batch, every sequence under its own
+    candidate: the prompts enter the caches (prefill), then every step embeds the last tokens, runs the blocks on one row per
+    sequence, multiplies by the head and draws the next token from the uniforms in `u`.
+
+    embed  [vocab, hidden] token embeddings (default: the head's rows), positions [n, hidden] learned positions or None.
+    temperature, top_k, top_p, min_p: a number for all sequences or one per sequence; None: no limit.
+    Everything a step reads lies on the device, so one captured graph replays every step; the caller fills `u` before each
+    draw and reads `tokens` after it."""
+
+    def __init__(self, model, max_new, embed=None, positions=None, temperature=1.0, top_k=None, top_p=None, min_p=None,
+                 page_size=64):
+        d = self.d = model.d
+        w, dev = d.w, d.device
+        S = self.S = d.batch.S
+        lens = np.diff(d.batch.host["cu"])
+        if (lens < 1).any():
+            raise ValueError("every sequence needs a prompt of at least one token")
+        if len({(blk.blk.n_kv_heads, blk.blk.head_dim) for blk in model.blocks}) != 1:
+            raise ValueError("the blocks' caches differ in heads or head dimension")
+        self.embed = d.head if embed is None else embed
+        self.positions = positions
+        self.hidden = self.embed.shape[1]
+        b0 = model.blocks[0].blk
+        self.cache = DeviceCache(len(model.blocks), S, int(lens.max()) + int(max_new), b0.n_kv_heads, b0.head_dim, d.dtype, dev,
+                                 page_size)
+        self.lens = torch.from_numpy(lens.astype(np.int32)).to(dev)
+        self.last = torch.from_numpy((d.batch.host["cu"][1:] - 1).astype(np.int32)).to(dev)
+        # the same layers, weights and candidates on one row per sequence
+        self.rows = copy.copy(d)
+        self.rows.batch = DeviceBatch(np.arange(S + 1), w.seq_cand, w.cand_dir, w.cand_sign, w.dir_seed, dev)
+        self.rows.Y = [torch.empty((S, y.shape[1]), device=dev, dtype=y.dtype) for y in d.Y]
+        self.plain = DeviceBatch(np.arange(S + 1), np.full(S, -1), np.zeros(0), np.zeros(0), np.zeros(0, np.uint64), dev)
+        ws = zb.zo_probe_linear_workspace_bytes(S, S, 0, d.head.shape[0], self.hidden, 1, 0, _dt(d.dtype))
+        for l in d.layers:
+            R = l.bank.R_used if l.bank is not None else 0
+            ws = max(ws, zb.zo_probe_linear_workspace_bytes(S, S, self.rows.batch.K, l.m, l.n, w.r, R, _dt(d.dtype)))
+        self.rows.ws_bytes, self.rows.ws = ws, torch.empty(max(ws, 256), device=dev, dtype=torch.uint8)
+        self.prompt_blocks = [CachedBlock(d, blk.blk, blk.base, c, True) for blk, c in zip(model.blocks, self.cache.structs)]
+        self.blocks = [CachedBlock(self.rows, blk.blk, blk.base, c, False) for blk, c in zip(model.blocks, self.cache.structs)]
+        self.gf, self.bf = model.gf, model.bf
+        new = lambda shape, dt: torch.empty(shape, device=dev, dtype=dt)
+        self.prompt_final, self.prompt_last = new((d.batch.T, self.hidden), _tt(d.dtype)), new((S, self.hidden), _tt(d.dtype))
+        self.x, self.final = (new((S, self.hidden), _tt(d.dtype)) for _ in range(2))
+        self.logits = new((S, d.head.shape[0]), torch.float32)
+        self.tokens, self.n_kept = new(S, torch.int32), new(S, torch.int32)
+        self.prob, self.u = new(S, torch.float32), torch.zeros(S, device=dev, dtype=torch.float32)
+        each = lambda v, dt: None if v is None else torch.from_numpy(np.broadcast_to(np.asarray(v, dt), (S,)).copy()).to(dev)
+        self.temperature, self.top_k = each(temperature, np.float32), each(top_k, np.int32)
+        self.top_p, self.min_p = each(top_p, np.float32), each(min_p, np.float32)
+        self.sample_bytes = zb.zo_sample_workspace_bytes(S, d.head.shape[0], zb.ZO_F32)
+        self.sample_ws = new(max(self.sample_bytes, 256), torch.uint8)
+        self.graph = None
+
+    def _blocks(self, blocks, x, out, stream):
+        res = None
+        for blk in blocks:
+            x, res = blk.forward(x, stream, res, last_sum=False)
+        blocks[-1].add_norm(x, res, self.gf, self.bf, None, out, stream)
+
+    def _draw(self, final, stream):
+        """Logits of the rows of `final` and the next tokens."""
+        d, h = self.d, self.d.head
+        zb.zo_probe_linear(self.plain.struct, final, final.stride(0), h, h.stride(0), None, h.shape[0], h.shape[1],
+                           _dt(d.dtype), 1, 0.0, 0, None, 0, self.logits, self.logits.stride(0), zb.ZO_F32, self.rows.ws,
+                           self.rows.ws_bytes, stream)
+        zb.zo_sample(self.logits, self.logits.stride(0), self.S, h.shape[0], zb.ZO_F32, self.temperature, self.top_k,
+                     self.top_p, self.min_p, self.u, self.tokens, self.prob, self.n_kept, self.sample_ws, self.sample_bytes,
+                     stream)
+
+    def prefill(self, stream=None):
+        """Runs the prompts (the workload's input rows) into the caches and draws every sequence's first token."""
+        self.cache.kv_len.copy_(self.lens)
+        self._blocks(self.prompt_blocks, self.d.X, self.prompt_final, stream)
+        f = self.prompt_final
+        zb.zo_embed_rows(self.last, None, self.S, f, f.stride(0), f.shape[0], None, 0, 0, self.hidden, _dt(self.d.dtype),
+                         self.prompt_last, self.hidden, None, stream)
+        self._draw(self.prompt_last, stream)
+
+    def step(self, stream=None):
+        """Appends the last tokens to their sequences and draws the next ones."""
+        e, p = self.embed, self.positions
+        kv = self.cache.kv_len   # (the new row's position before the call, the cache's length after it)
+        zb.zo_embed_rows(self.tokens, kv, self.S, e, e.stride(0), e.shape[0], p, 0 if p is None else p.stride(0),
+                         0 if p is None else p.shape[0], self.hidden, _dt(self.d.dtype), self.x, self.hidden, kv, stream)
+        self._blocks(self.blocks, self.x, self.final, stream)
+        self._draw(self.final, stream)
+
+    def capture(self):
+        """Captures one step into a HIP graph after an eager warm-up step on a side stream, which configures the kernels.
+        The warm-up step is a real step: call prefill() afterwards."""
+        side = torch.cuda.Stream(device=self.d.device)
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            self.step(side)
+        torch.cuda.current_stream().wait_stream(side)
+        torch.cuda.synchronize()
+        self.graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(self.graph):
+            self.step(torch.cuda.current_stream())
         return self.graph
 
     def replay(self):
