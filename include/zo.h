@@ -483,8 +483,9 @@ int32_t zo_cache_append(const zo_batch* batch, const void* Q, int64_t ldq, const
  * Attention of new rows over the cache (their own keys and values stored by zo_cache_append first):
  *   O[t, h] = sum_j softmax_j(scale * <Q[t, h], K[j, g]>) V[j, g],   g = h / (n_heads / n_kv_heads),
  *   j over the positions 0 .. pos(t) of the row's sequence
- * A row that sees no position (kv_len 0, or only pages outside the pool) gets zeros.  Laid out for one
- * row per sequence; several rows of a sequence each read its cache.
+ * A row that sees no position (kv_len 0, or only pages outside the pool) gets zeros; rows behind the last
+ * sequence are left as they were.  O must not overlap Q or the pools.  Laid out for one row per sequence; several rows of
+ * a sequence each read its cache.
  * ZO_BF16: head_dim 64, 128 or 256; products on bf16 MFMA with fp32 accumulation, softmax in fp32, weights
  * rounded to bf16 before the second product.  ZO_F32: head_dim <= 256, fp32 throughout.
  * A long row is cut into ranges that are joined afterwards; the ranges depend on the row's own
@@ -515,7 +516,8 @@ int32_t zo_attention_paged(const zo_batch* batch, const void* Q, int64_t ldq, in
  * -infinity: token -1, prob 0, n_kept 0.  u is clamped to [0, 1] (NaN: 0).
  *   temperature, u  fp32 [n_rows];  top_k int32 [n_rows], top_p, min_p fp32 [n_rows], each may be NULL: no limit
  *   tokens int32 [n_rows];  prob fp32 [n_rows] and n_kept int32 [n_rows], each may be NULL
- * Weights and their sums are formed in 64 bits.  vocab up to 2^19.  The logits need no alignment beyond their type's.
+ * Weights and their sums are formed in 64 bits; a weight below 2^-1000 of the largest is none.  vocab up to 2^19.  The logits
+ * need no alignment beyond their type's.  The kernel's scratch lies in LDS: the query returns 0, and workspace may be NULL.
  */
 size_t zo_sample_workspace_bytes(int32_t n_rows, int32_t vocab, zo_dtype dtype);
 

@@ -94,7 +94,8 @@ def kept_tokens(z, temperature, top_k, top_p, min_p):
     n_k = len(order) if top_k <= 0 else min(top_k, len(order))
     n = n_k
     if top_p < 1:
-        n = sum(1 for before in np.concatenate([[0.0], np.cumsum(w[:n_k])[:-1]]) if before < top_p * w[:n_k].sum())
+        before = np.concatenate([[0.0], np.cumsum(w[:n_k])[:-1]])
+        n = int((before < top_p * w[:n_k].sum()).sum())
     if min_p > 0:
         n = min(n, int((w >= min_p).sum()))
     n = max(n, 1)

@@ -25,6 +25,7 @@ int32_t fail(zo_status st, const char* fmt, ...) {
   } while (0)
 
 constexpr int64_t kMaxLd = (int64_t)1 << 22;
+constexpr int64_t kMaxThreads = (int64_t)1 << 31;   // of a launch along one dimension
 constexpr int kMaxVocab = 1 << 19;   // (2^44 per weight of 64-bit bin sums)
 
 int32_t check_cache(const zo_batch* b, const zo_cache* c) {
@@ -75,6 +76,12 @@ zo::CacheDev to_dev(const zo_cache* c) {
   return d;
 }
 
+// Whether `items` times the threads of each fit one launch.
+int32_t check_launch(const char* what, int64_t items, int64_t threads) {
+  if (items > kMaxThreads / threads) return fail(ZO_ERR_UNSUPPORTED, "%s = %lld: up to %lld fit one call", what, (long long)items, (long long)(kMaxThreads / threads));
+  return ZO_OK;
+}
+
 // A matrix of rows that need no alignment beyond their type's.
 int32_t check_rows(const char* name, const void* p, int64_t ld, int cols, zo_dtype dt) {
   if (ld < cols || ld > kMaxLd)
@@ -123,6 +130,7 @@ int32_t zo_cache_append(const zo_batch* batch, const void* Q, int64_t ldq, const
   if ((((uintptr_t)gamma_q | (uintptr_t)gamma_k) & 3u) != 0) return fail(ZO_ERR_SHAPE, "gamma_q / gamma_k: pointer misaligned");
   if (!(norm_eps >= 0.0f)) return fail(ZO_ERR_SHAPE, "norm_eps = %g", (double)norm_eps);
   if (batch->n_tokens == 0) return ZO_OK;
+  if (int32_t st = check_launch("n_tokens * (n_heads + 2 * n_kv_heads)", (int64_t)batch->n_tokens * (n_heads + 2 * cache->n_kv_heads), 64)) return st;
   if (!Q || !K || !V || !Qout) return fail(ZO_ERR_NULL, "Q, K, V or Qout is NULL");
   if (Qout == Q && ldqo != ldq) return fail(ZO_ERR_SHAPE, "Qout is Q, but with another leading dimension");
   const zo_dtype dt = cache->dtype;
@@ -158,6 +166,7 @@ int32_t zo_attention_paged(const zo_batch* batch, const void* Q, int64_t ldq, in
   if (dh > 256) return fail(ZO_ERR_UNSUPPORTED, "the fp32 kernel covers head_dim <= 256 (head_dim = %d)", dh);
   const int T = batch->n_tokens;
   if (T == 0) return ZO_OK;
+  if (int32_t st = check_launch("n_tokens * n_heads", (int64_t)T * n_heads, 256)) return st;
   if (!Q || !O) return fail(ZO_ERR_NULL, "Q or O is NULL");
   if (int32_t st = zo::matrix_validate("Q", Q, ldq, n_heads * dh, dt)) return st;
   if (int32_t st = zo::matrix_validate("O", O, ldo, n_heads * dh, dt)) return st;
@@ -185,6 +194,7 @@ int32_t zo_sample(const void* logits, int64_t ld, int32_t n_rows, int32_t vocab,
   if (vocab > kMaxVocab) return fail(ZO_ERR_UNSUPPORTED, "vocab = %d: up to %d are covered", vocab, kMaxVocab);
   if (dtype != ZO_F32 && dtype != ZO_BF16) return fail(ZO_ERR_UNSUPPORTED, "dtype %d", (int)dtype);
   if (n_rows == 0) return ZO_OK;
+  if (int32_t st = check_launch("n_rows", n_rows, 1024)) return st;
   if (!logits || !temperature || !u || !tokens) return fail(ZO_ERR_NULL, "logits, temperature, u or tokens is NULL");
   if (int32_t st = check_rows("logits", logits, ld, vocab, dtype)) return st;
   if (int32_t st = check_workspace(workspace, workspace_bytes, zo_sample_workspace_bytes(n_rows, vocab, dtype))) return st;
@@ -203,6 +213,7 @@ int32_t zo_embed_rows(const int32_t* tokens, const int32_t* pos, int32_t n_rows,
     return fail(ZO_ERR_SHAPE, "n_rows = %d, vocab = %d, n_pos = %d, d = %d", n_rows, vocab, n_pos, d);
   if (dtype != ZO_F32 && dtype != ZO_BF16) return fail(ZO_ERR_UNSUPPORTED, "dtype %d", (int)dtype);
   if (n_rows == 0) return ZO_OK;
+  if (int32_t st = check_launch("n_rows", n_rows, 256)) return st;
   if (!tokens) return fail(ZO_ERR_NULL, "tokens is NULL");
   if (!pos && (E_pos || pos_next)) return fail(ZO_ERR_NULL, "pos is NULL");
   if (d > 0) {

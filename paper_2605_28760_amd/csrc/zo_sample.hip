@@ -34,7 +34,7 @@ constexpr int kLast = kBins - 1;
 constexpr int kPieces = 4;           // loads of a wave under way, four neighbouring tokens a lane each
 constexpr int kStrip = kPieces * 4 * kWave;
 constexpr int kMaxVocab = 1 << 19;
-constexpr int kMaxStrips = kMaxVocab / kStrip;
+constexpr int kMaxStrips = kMaxVocab / kStrip + 1;   // (a row may begin inside one)
 constexpr int kList = 4096;          // tokens that fit in LDS
 constexpr int kShort = 512;          // tokens that are ranked by comparing each with each (7 us; 1024 take 27, cutting a bin 18)
 
@@ -64,11 +64,11 @@ __device__ __forceinline__ void unpack(const uint2& v, float (&x)[4]) {
   x[0] = __uint_as_float(v.x << 16); x[1] = __uint_as_float(v.x & 0xFFFF0000u);
   x[2] = __uint_as_float(v.y << 16); x[3] = __uint_as_float(v.y & 0xFFFF0000u);
 }
-// Four from `at` of a row of any alignment and end: -infinity behind it.
+// Four from `at` of a row, one by one: -infinity before its begin and behind its end.
 template <typename Tio>
 __device__ __forceinline__ void four(const Tio* z, int at, int V, float (&x)[4]) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) x[j] = at + j < V ? ld_logit(z, at + j) : -INFINITY;
+  for (int j = 0; j < 4; ++j) x[j] = (unsigned)(at + j) < (unsigned)V ? ld_logit(z, at + j) : -INFINITY;
 }
 
 // Adding it leaves the nearest integer in the low word.
@@ -195,19 +195,25 @@ struct Row {
   Shared& s;
   const Tio* z;
   int V, tid, lane, wave;
-  bool vec;
+  int shift;   // tokens by which the row begins behind a multiple of four tokens' size: strips count from there
+
+  __device__ __forceinline__ int n_strips() const { return (V + shift + kStrip - 1) / kStrip; }
+  // the lane's first token in piece u of a strip
+  __device__ __forceinline__ int first(int st, int u) const { return st * kStrip + u * (4 * kWave) + lane * 4 - shift; }
 
   // f(x, first index) for every four tokens of a strip of kStrip tokens, strip by strip of this wave's share, then
   // done(strip).  A whole strip's loads are under way together, and those of the next one under its work.
   template <class F, class Done>
   __device__ __forceinline__ void strips(F f, Done done) const {
-    const int n = (V + kStrip - 1) / kStrip, whole = vec ? V / kStrip : 0;
+    const int n = n_strips(), whole = (V + shift) / kStrip;
     typedef typename Raw<Tio>::type R;
-    int st = wave;
+    const bool begins = shift > 0 && wave == 0;   // the first strip is not whole
+    int st = begins ? kWaves : wave;
+    const Tio* const base = z - shift;
     R next[kPieces];
     auto load = [&](int at) __attribute__((always_inline)) {
 #pragma unroll
-      for (int u = 0; u < kPieces; ++u) next[u] = *reinterpret_cast<const R*>(z + at * kStrip + u * (4 * kWave) + lane * 4);
+      for (int u = 0; u < kPieces; ++u) next[u] = *reinterpret_cast<const R*>(base + at * kStrip + u * (4 * kWave) + lane * 4);
     };
     if (st < whole) load(st);
     for (; st < whole; st += kWaves) {
@@ -219,18 +225,17 @@ struct Row {
       for (int u = 0; u < kPieces; ++u) {
         float x[4];
         unpack(raw[u], x);
-        f(x, st * kStrip + u * (4 * kWave) + lane * 4);
+        f(x, first(st, u));
       }
       done(st);
     }
-    for (; st < n; st += kWaves) {
+    for (int rest = begins ? 0 : st; rest < n; rest = begins && rest == 0 ? st : rest + kWaves) {   // the row's begin and end
       for (int u = 0; u < kPieces; ++u) {
         float x[4];
-        const int at = st * kStrip + u * (4 * kWave) + lane * 4;
-        four(z, at, V, x);
-        f(x, at);
+        four(z, first(rest, u), V, x);
+        f(x, first(rest, u));
       }
-      done(st);
+      done(rest);
     }
   }
   template <class F>
@@ -241,16 +246,16 @@ struct Row {
   template <class F>
   __device__ __forceinline__ void whole_strips(F f) const {
     float x[kPieces][4];
-    int u = 0, first = 0;
+    int u = 0, begin = 0;
     strips(
         [&](const float (&y)[4], int at) {
-          if (u == 0) first = at;
+          if (u == 0) begin = at;
 #pragma unroll
           for (int j = 0; j < 4; ++j) x[u & (kPieces - 1)][j] = y[j];
           ++u;
         },
         [&](int st) {
-          f(x, first, st);
+          f(x, begin, st);
           u = 0;
         });
   }
@@ -402,7 +407,7 @@ __device__ __forceinline__ void list_index(Shared& s, int tid, int lane, int wav
 template <typename Tio, class Is>
 __device__ __forceinline__ void nth_index(const Row<Tio>& rw, u64 n, Is is) {
   Shared& s = rw.s;
-  const int strips = (rw.V + kStrip - 1) / kStrip;
+  const int strips = rw.n_strips();
   uint32_t c = 0;
   __syncthreads();
   rw.strips(
@@ -427,7 +432,7 @@ __device__ __forceinline__ void nth_index(const Row<Tio>& rw, u64 n, Is is) {
     u64 seen = s.n_before;
     for (int u = 0; u < kPieces; ++u) {
       float x[4];
-      const int at = s.bin * kStrip + u * (4 * kWave) + rw.lane * 4;
+      const int at = rw.first(s.bin, u);
       four(rw.z, at, rw.V, x);
       int here = 0;
 #pragma unroll
@@ -460,8 +465,8 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
   Shared& s = *reinterpret_cast<Shared*>(lds);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int row = blockIdx.x, V = a.V;
-  Row<Tio> rw{s, (const Tio*)a.z + (int64_t)row * a.ld, V, tid, lane, wave, false};
-  rw.vec = ((uintptr_t)rw.z & (4 * sizeof(Tio) - 1)) == 0;   // (a row whose four tokens do not start on their size goes one by one)
+  Row<Tio> rw{s, (const Tio*)a.z + (int64_t)row * a.ld, V, tid, lane, wave, 0};
+  rw.shift = (int)((uintptr_t)rw.z % (4 * sizeof(Tio)) / sizeof(Tio));
   const float temp = a.temperature[row];
   const int k = a.top_k ? a.top_k[row] : 0;
   const float p = a.top_p ? a.top_p[row] : 1.f;
@@ -825,7 +830,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
     }
     return;
   }
-  const int strips = (V + kStrip - 1) / kStrip;
+  const int strips = rw.n_strips();
   u64 number = 0;
   __syncthreads();   // (the strips' sums take the list's place)
   float* const packed = s.packed[wave];
@@ -918,7 +923,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
   for (int u = 0; u < kPieces; ++u) {
     float x[4];
     double w[4], run = 0.0;
-    const int first = at * kStrip + u * (4 * kWave) + lane * 4;
+    const int first = rw.first(at, u);
     four(rw.z, first, V, x);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {

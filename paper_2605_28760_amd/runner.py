@@ -323,7 +323,8 @@ class DecodeDriver:
     embed  [vocab, hidden] token embeddings (default: the head's rows), positions [n, hidden] learned positions or None.
     temperature, top_k, top_p, min_p: a number for all sequences or one per sequence; None: no limit.
     Everything a step reads lies on the device, so one captured graph replays every step; the caller fills `u` before each
-    draw and reads `tokens` after it."""
+    draw and reads `tokens` after it.  The caches have room for max_new tokens behind the longest prompt: what follows them is
+    not stored."""
 
     def __init__(self, model, max_new, embed=None, positions=None, temperature=1.0, top_k=None, top_p=None, min_p=None,
                  page_size=64):
@@ -337,6 +338,9 @@ class DecodeDriver:
             raise ValueError("the blocks' caches differ in heads or head dimension")
         self.embed = d.head if embed is None else embed
         self.positions = positions
+        for what, t in (("embed", self.embed), ("positions", positions)):
+            if t is not None and (t.dtype != _tt(d.dtype) or t.dim() != 2 or t.shape[1] != d.head.shape[1] or t.stride(1) != 1):
+                raise ValueError("%s: rows of %d values of the model's type are needed" % (what, d.head.shape[1]))
         self.hidden = self.embed.shape[1]
         b0 = model.blocks[0].blk
         self.cache = DeviceCache(len(model.blocks), S, int(lens.max()) + int(max_new), b0.n_kv_heads, b0.head_dim, d.dtype, dev,

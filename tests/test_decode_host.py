@@ -137,6 +137,15 @@ def test_embed_rows_refusals():
     emb(T=0, tok=None)
 
 
+def test_calls_beyond_one_launch_are_refused():
+    big = zb.make_batch((1 << 21) + 1, FAKE, FAKE, None, None, None, None, n_seqs=3, n_cands=0, n_dirs=0)
+    assert _status(_append, big, _cache(n_kv_heads=8), H=8, ldq=4096, ldk=4096, ldv=4096, ldqo=4096) == zb.ZO_ERR_UNSUPPORTED
+    assert _status(_attend, big) == zb.ZO_ERR_UNSUPPORTED
+    assert _status(zb.zo_sample, FAKE, 10, (1 << 21) + 1, 10, zb.ZO_F32, FAKE, None, None, None, FAKE, FAKE, None, None, None, 0) == \
+        zb.ZO_ERR_UNSUPPORTED
+    assert _status(zb.zo_embed_rows, FAKE, None, (1 << 23) + 1, FAKE, 8, 10, None, 0, 0, 8, zb.ZO_F32, FAKE, 8, None) == zb.ZO_ERR_UNSUPPORTED
+
+
 def test_make_cache_checks_its_tensors():
     torch = pytest.importorskip("torch")
     K = torch.zeros(4, 2, 16, 8)

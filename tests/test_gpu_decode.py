@@ -103,7 +103,7 @@ class Setup:
                     p = np.exp(s - s.max())
                     p /= p.sum()
                     want, size = p @ v, p @ np.abs(v)
-                    ds = (dh + 3) * U * abs(scale) * (np.abs(k) @ np.abs(x)).max()
+                    ds = (dh + 3) * U * abs(scale) * (np.abs(k[s > -np.inf]) @ np.abs(x)).max()
                     tol = (2 * ds + (len(p) + 16) * U + (h if self.dtype == "bf16" else 0)) * size + h * np.abs(want)
                     err = np.abs(got[t, head] - want)
                     assert (err <= tol).all(), (t, i, pos, head, float((err / tol).max()))
@@ -215,6 +215,34 @@ def test_attention_of_large_scores(scale, shift):
     s = Setup(13, "f32", 4, 2, 64, 16, [1] * 3, [50, 257, 600])
     s.K += shift
     s.check_attend(s.attend(scale), scale)
+
+
+@pytest.mark.parametrize("dtype,dh", [("bf16", 128), ("f32", 64)])
+def test_keys_at_minus_infinity_have_no_weight(dtype, dh):
+    """Whole steps, whole ranges and only some heads' scores at -infinity before the first finite one."""
+    kv = [45, 300, 700, 1400]
+    s = Setup(16, dtype, 4, 2, dh, 16, [1] * 4, kv)
+    s.q[:, 0::dh] = s.q[:, 0::dh].abs() + 0.1           # every head's first value: positive ..
+    for i, n in enumerate((40, 270, 150, 1390)):
+        for p in range(n):
+            s.K[int(s.table[i, p // 16]), (0 if i == 2 else slice(None)), p % 16, 0] = float("-inf")   # .. times -infinity
+    got = _np(s.attend())
+    assert np.isfinite(got[:, :4 * dh]).all()
+    s.check_attend(s.out)
+
+
+def test_thousands_of_sequences():
+    """More sequences than one look at the bounds holds, empty ones among them."""
+    rng = np.random.default_rng(17)
+    rows = rng.integers(0, 2, 4500)
+    kv = rows + rng.integers(0, 30, 4500)
+    s = Setup(17, "f32", 1, 1, 64, 16, rows, kv, extra_rows=3)
+    K0, V0 = _np(s.K), _np(s.V)
+    s.append(None, None, 1e4, out=s.out)
+    q, K, V = od.cache_append(_np(s.q)[:s.T - 3], _np(s.k), _np(s.v), s.cu, 1, None, None, 0.0, 1e4, K0, V0, s.table, s.kv)
+    assert (_np(s.V) == V).all() and (np.abs(_np(s.K) - K) <= 1e-5).all() and (np.abs(_np(s.out)[:s.T - 3] - q) <= 1e-5).all()
+    s.check_attend(s.attend())
+    assert (_np(s.out)[s.T - 3:] == 7).all()
 
 
 def test_rows_do_not_depend_on_the_batch_or_the_table():
@@ -376,6 +404,26 @@ def test_sample_rows_of_any_alignment(dtype, pad):
     buf = torch.from_numpy(rng.normal(size=(5, 2047 + pad)) * 2).to(DEV).to(TT[dtype])
     z = buf[:, pad:]
     _check_draw(z, [1.0] * 5, [50] * 5, [0.9] * 5, None, rng.uniform(size=5))
+
+
+@pytest.mark.parametrize("dtype,pad,V", [("bf16", 1, 9001), ("bf16", 2, 1023), ("f32", 3, 5121), ("f32", 2, 1022), ("f32", 1, 1 << 19),
+                                         ("bf16", 3, 1 << 19)])
+def test_sample_rows_that_begin_anywhere(dtype, pad, V):
+    """Every row begins at another place of a 16-byte piece; what lies around a row must not be drawn."""
+    rng = np.random.default_rng(V + pad)
+    T = 4 if V > 10000 else 8
+    buf = torch.full((T * (V + pad) + 8,), 1e9, device=DEV).to(TT[dtype])
+    z = buf[pad:pad + T * (V + pad)].view(T, V + pad)[:, :V]
+    z.copy_(torch.from_numpy(rng.normal(size=(T, V)) * 2))
+    u = rng.uniform(size=T)
+    u[0], u[-1] = 0.0, 1.0
+    one = [1.0] * T
+    _check_draw(z, one, None, None, None, u)
+    _check_draw(z, one, [30] * T, None, None, u)
+    _check_draw(z, one, None, [0.3] * T, None, u)
+    _check_draw(z, one, None, [0.97] * T, None, u)
+    _check_draw(z, one, None, None, [0.02] * T, u)
+    _check_draw(z, [0.0] * T, None, None, None, u)
 
 
 def test_sample_draws_every_kept_token_in_proportion():

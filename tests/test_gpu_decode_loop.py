@@ -129,3 +129,10 @@ def test_driver_refusals():
     w.cu_seqlens = np.array([0, 0, 6], np.int32)
     with pytest.raises(ValueError, match="prompt"):
         DecodeDriver(DeviceModel(DeviceWorkload(w, DEV)), 2)
+    w.cu_seqlens = np.array([0, 3, 6], np.int32)
+    model = DeviceModel(DeviceWorkload(w, DEV))
+    for bad in (torch.zeros(50, 32, device=DEV).bfloat16(), torch.zeros(50, 31, device=DEV), torch.zeros(32, 50, device=DEV).t()):
+        with pytest.raises(ValueError, match="embed"):
+            DecodeDriver(model, 2, bad)
+        with pytest.raises(ValueError, match="positions"):
+            DecodeDriver(model, 2, None, bad)
