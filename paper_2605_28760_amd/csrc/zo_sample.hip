@@ -981,28 +981,32 @@ __global__ __launch_bounds__(256) void k_embed_rows_any(EmbedArgs a) {
   }
 }
 
-// Rows whose pieces of 16 bytes are aligned: a workgroup per row, four pieces of a lane under way.  16384 rows of 5120 with
-// positions: 74 us (4.8 TB/s), element by element 180; few rows: the latency of two loads that depend on each other.
+// Rows whose pieces of 16 bytes are aligned: 2^log_lanes threads per row, about as many as it has pieces, four pieces of a thread
+// under way.  16384 rows of 5120 with positions: 75 us (4.8 TB/s), element by element 180; few rows: the latency of two loads
+// that depend on each other.
 template <typename Tio>
-__global__ __launch_bounds__(256) void k_embed_rows(EmbedArgs a) {
+__global__ __launch_bounds__(256) void k_embed_rows(EmbedArgs a, int log_lanes) {
   constexpr int kDeep = 4, kPer = 16 / sizeof(Tio);
-  const int t = blockIdx.x;
+  const int lanes = 1 << log_lanes, lane = threadIdx.x & (lanes - 1);
+  const int64_t row = (int64_t)blockIdx.x * (256 >> log_lanes) + (threadIdx.x >> log_lanes);
+  const bool there = row < a.T;
+  const int t = there ? (int)row : 0;
   const int tok = a.tokens[t], pos = a.pos ? a.pos[t] : 0;
   const u32x4* e = (unsigned)tok < (unsigned)a.vocab ? (const u32x4*)((const Tio*)a.E + (int64_t)tok * a.lde) : nullptr;
   const u32x4* q = a.Epos && (unsigned)pos < (unsigned)a.n_pos ? (const u32x4*)((const Tio*)a.Epos + (int64_t)pos * a.ldp) : nullptr;
   u32x4* x = (u32x4*)((Tio*)a.X + (int64_t)t * a.ldx);
-  const int n = a.d / kPer;
-  for (int i0 = threadIdx.x; i0 < n; i0 += kDeep * 256) {
+  const int n = there ? a.d / kPer : 0;
+  for (int i0 = lane; i0 < n; i0 += kDeep * lanes) {
     u32x4 v[kDeep], w[kDeep];
 #pragma unroll
     for (int u = 0; u < kDeep; ++u) {
-      const int i = i0 + u * 256;
+      const int i = i0 + u * lanes;
       v[u] = e && i < n ? e[i] : u32x4{0u, 0u, 0u, 0u};
       w[u] = q && i < n ? q[i] : u32x4{0u, 0u, 0u, 0u};
     }
 #pragma unroll
     for (int u = 0; u < kDeep; ++u) {
-      const int i = i0 + u * 256;
+      const int i = i0 + u * lanes;
       if (i >= n) break;
       if (q) {
 #pragma unroll
@@ -1018,8 +1022,8 @@ __global__ __launch_bounds__(256) void k_embed_rows(EmbedArgs a) {
     }
   }
   if (a.pos_next) {
-    __syncthreads();   // (pos_next may be pos: every wave has read it)
-    if (threadIdx.x == 0) a.pos_next[t] = (int32_t)((uint32_t)pos + 1u);
+    __syncthreads();   // (pos_next may be pos: every thread has read it)
+    if (there && lane == 0) a.pos_next[t] = (int32_t)((uint32_t)pos + 1u);
   }
 }
 
@@ -1046,9 +1050,11 @@ hipError_t launch_embed_rows(const EmbedArgs& a, hipStream_t st) {
   const int size = a.bf16 ? 2 : 4;
   auto aligned = [&](const void* p, int64_t ld) { return ((uintptr_t)p & 15u) == 0 && ld * size % 16 == 0; };
   const bool wide = a.d * size % 16 == 0 && aligned(a.E, a.lde) && aligned(a.X, a.ldx) && (!a.Epos || aligned(a.Epos, a.ldp));
-  const dim3 grid(a.T);
-  if (wide && a.bf16) k_embed_rows<bf16_t><<<grid, 256, 0, st>>>(a);
-  else if (wide) k_embed_rows<float><<<grid, 256, 0, st>>>(a);
+  int log_lanes = 3;
+  while (log_lanes < 8 && (16 << log_lanes) < a.d * size) ++log_lanes;
+  const dim3 grid(a.T), rows((unsigned)(((int64_t)a.T + (256 >> log_lanes) - 1) / (256 >> log_lanes)));
+  if (wide && a.bf16) k_embed_rows<bf16_t><<<rows, 256, 0, st>>>(a, log_lanes);
+  else if (wide) k_embed_rows<float><<<rows, 256, 0, st>>>(a, log_lanes);
   else if (a.bf16) k_embed_rows_any<bf16_t><<<grid, 256, 0, st>>>(a);
   else k_embed_rows_any<float><<<grid, 256, 0, st>>>(a);
   return hipGetLastError();
