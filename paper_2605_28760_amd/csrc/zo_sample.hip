@@ -34,7 +34,7 @@ constexpr int kLast = kBins - 1;
 constexpr int kPieces = 4;           // loads of a wave under way, four neighbouring tokens a lane each
 constexpr int kStrip = kPieces * 4 * kWave;
 constexpr int kMaxVocab = 1 << 19;
-constexpr int kMaxStrips = kMaxVocab / kStrip + 1;   // (a row may begin inside one)
+constexpr int kMaxStrips = kMaxVocab / kStrip;
 constexpr int kList = 4096;          // tokens that fit in LDS
 constexpr int kShort = 512;          // tokens that are ranked by comparing each with each (7 us; 1024 take 27, cutting a bin 18)
 
@@ -53,22 +53,24 @@ __device__ __forceinline__ uint32_t key_of(float z) {
 }
 __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
 
-// Four neighbouring logits as they lie in memory.
+// Four neighbouring logits as they lie in memory, of no more than a logit's alignment: one load all the same, and a row's strips
+// and the order of its sums do not depend on where it begins.
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 template <typename Tio> struct Raw;
-template <> struct Raw<float> { typedef float4 type; };
-template <> struct Raw<bf16_t> { typedef uint2 type; };
-__device__ __forceinline__ void unpack(const float4& v, float (&x)[4]) {
+template <> struct Raw<float> { typedef f32x4 type; typedef f32x4 __attribute__((aligned(4))) in_memory; };
+template <> struct Raw<bf16_t> { typedef u32x2 type; typedef u32x2 __attribute__((aligned(2))) in_memory; };
+__device__ __forceinline__ void unpack(const f32x4& v, float (&x)[4]) {
   x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
 }
-__device__ __forceinline__ void unpack(const uint2& v, float (&x)[4]) {
+__device__ __forceinline__ void unpack(const u32x2& v, float (&x)[4]) {
   x[0] = __uint_as_float(v.x << 16); x[1] = __uint_as_float(v.x & 0xFFFF0000u);
   x[2] = __uint_as_float(v.y << 16); x[3] = __uint_as_float(v.y & 0xFFFF0000u);
 }
-// Four from `at` of a row, one by one: -infinity before its begin and behind its end.
+// Four from `at` of a row, one by one: -infinity behind its end.
 template <typename Tio>
 __device__ __forceinline__ void four(const Tio* z, int at, int V, float (&x)[4]) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) x[j] = (unsigned)(at + j) < (unsigned)V ? ld_logit(z, at + j) : -INFINITY;
+  for (int j = 0; j < 4; ++j) x[j] = at + j < V ? ld_logit(z, at + j) : -INFINITY;
 }
 
 // Adding it leaves the nearest integer in the low word.
@@ -195,25 +197,23 @@ struct Row {
   Shared& s;
   const Tio* z;
   int V, tid, lane, wave;
-  int shift;   // tokens by which the row begins behind a multiple of four tokens' size: strips count from there
 
-  __device__ __forceinline__ int n_strips() const { return (V + shift + kStrip - 1) / kStrip; }
+  __device__ __forceinline__ int n_strips() const { return (V + kStrip - 1) / kStrip; }
   // the lane's first token in piece u of a strip
-  __device__ __forceinline__ int first(int st, int u) const { return st * kStrip + u * (4 * kWave) + lane * 4 - shift; }
+  __device__ __forceinline__ int first(int st, int u) const { return st * kStrip + u * (4 * kWave) + lane * 4; }
 
   // f(x, first index) for every four tokens of a strip of kStrip tokens, strip by strip of this wave's share, then
   // done(strip).  A whole strip's loads are under way together, and those of the next one under its work.
   template <class F, class Done>
   __device__ __forceinline__ void strips(F f, Done done) const {
-    const int n = n_strips(), whole = (V + shift) / kStrip;
+    const int n = n_strips(), whole = V / kStrip;
     typedef typename Raw<Tio>::type R;
-    const bool begins = shift > 0 && wave == 0;   // the first strip is not whole
-    int st = begins ? kWaves : wave;
-    const Tio* const base = z - shift;
+    typedef typename Raw<Tio>::in_memory R_mem;
+    int st = wave;
     R next[kPieces];
     auto load = [&](int at) __attribute__((always_inline)) {
 #pragma unroll
-      for (int u = 0; u < kPieces; ++u) next[u] = *reinterpret_cast<const R*>(base + at * kStrip + u * (4 * kWave) + lane * 4);
+      for (int u = 0; u < kPieces; ++u) next[u] = *reinterpret_cast<const R_mem*>(z + first(at, u));
     };
     if (st < whole) load(st);
     for (; st < whole; st += kWaves) {
@@ -229,13 +229,13 @@ struct Row {
       }
       done(st);
     }
-    for (int rest = begins ? 0 : st; rest < n; rest = begins && rest == 0 ? st : rest + kWaves) {   // the row's begin and end
+    if (st < n) {   // the row's end, not a whole strip
       for (int u = 0; u < kPieces; ++u) {
         float x[4];
-        four(z, first(rest, u), V, x);
-        f(x, first(rest, u));
+        four(z, first(st, u), V, x);
+        f(x, first(st, u));
       }
-      done(rest);
+      done(st);
     }
   }
   template <class F>
@@ -465,8 +465,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
   Shared& s = *reinterpret_cast<Shared*>(lds);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int row = blockIdx.x, V = a.V;
-  Row<Tio> rw{s, (const Tio*)a.z + (int64_t)row * a.ld, V, tid, lane, wave, 0};
-  rw.shift = (int)((uintptr_t)rw.z % (4 * sizeof(Tio)) / sizeof(Tio));
+  Row<Tio> rw{s, (const Tio*)a.z + (int64_t)row * a.ld, V, tid, lane, wave};
   const float temp = a.temperature[row];
   const int k = a.top_k ? a.top_k[row] : 0;
   const float p = a.top_p ? a.top_p[row] : 1.f;

@@ -426,6 +426,21 @@ def test_sample_rows_that_begin_anywhere(dtype, pad, V):
     _check_draw(z, [0.0] * T, None, None, None, u)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_sample_results_do_not_depend_on_where_a_row_begins(dtype):
+    """The same row at every place of a 16-byte piece, with a prefix that fits in LDS and one that does not: the same bits."""
+    rng = np.random.default_rng(12)
+    V, T = 30011, 8                                   # (an odd leading dimension: neighbouring rows begin at different places)
+    row = rng.normal(size=V)
+    z = torch.from_numpy(np.tile(row, (T, 1))).to(DEV).to(TT[dtype])
+    assert z.stride(0) == V
+    for u in rng.uniform(size=6):
+        for k, p, m in ((None, None, None), (None, [0.9] * T, None), (None, [0.2] * T, None), ([6000] * T, [0.95] * T, None),
+                        ([40] * T, [0.9] * T, None), (None, None, [0.01] * T)):
+            tok, prob, kept = _draw(z, [0.9] * T, k, p, m, [u] * T)
+            assert len(set(tok)) == len(set(prob)) == len(set(kept)) == 1
+
+
 def test_sample_draws_every_kept_token_in_proportion():
     V, T = 300, 4096
     rng = np.random.default_rng(4)
