@@ -488,7 +488,8 @@ int32_t zo_cache_append(const zo_batch* batch, const void* Q, int64_t ldq, const
  * sequence are left as they were.  O must not overlap Q or the pools.  Laid out for one row per sequence; several rows of
  * a sequence each read its cache.
  * ZO_BF16: head_dim 64, 128 or 256; products on bf16 MFMA with fp32 accumulation, softmax in fp32, weights
- * rounded to bf16 before the second product.  ZO_F32: head_dim <= 256, fp32 throughout.
+ * as the sum of two bf16 values in the second product (2^-15 of a weight is lost at most).  ZO_F32: head_dim <= 256,
+ * fp32 throughout.
  * A long row is cut into ranges that are joined afterwards; the ranges depend on the row's own
  * position alone, so its bits depend neither on the batch nor on the size of the page table.
  * The workspace holds the ranges' partial results: max_len is max_pages * page_size of the cache.

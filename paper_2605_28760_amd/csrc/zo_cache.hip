@@ -338,17 +338,28 @@ struct Bf16Step {
       for (int i = 0; i < 4; ++i) s[4 * hf + i] = acc[i];
     }
   }
-  // (the weights are rounded to bf16 here: half a step of 2^-8 each, averaged over the keys of a row)
+  // A weight takes two products: its upper 16 bits, and the rest rounded to bf16, so that 2^-15 of it is lost at most (2^-8 with
+  // one).  The rest counts 2^-20 of the weight more, so that it is none only where the weight is: zero times an infinite value
+  // would be NaN.
   __device__ __forceinline__ void values(const float (&p)[kScores], f32x4 (&o)[kCols]) const {
-    const u32x4 packed = {pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7])};
-    const bf16x8 pf = __builtin_bit_cast(bf16x8, packed);
+    u32x4 upper, rest;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t a = __float_as_uint(p[2 * j]), b = __float_as_uint(p[2 * j + 1]);
+      upper[j] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+      rest[j] = pack_bf16x2(__builtin_fmaf(p[2 * j], 1.0f + 0x1p-20f, -__uint_as_float(a & 0xFFFF0000u)),
+                            __builtin_fmaf(p[2 * j + 1], 1.0f + 0x1p-20f, -__uint_as_float(b & 0xFFFF0000u)));
+    }
+    const bf16x8 pu = __builtin_bit_cast(bf16x8, upper), pr = __builtin_bit_cast(bf16x8, rest);
 #pragma unroll
     for (int d = 0; d < kCols; ++d) {
       u32x4 w;
 #pragma unroll
       for (int j = 0; j < 4; ++j)   // column d of keys 2 j and 2 j + 1
         w[j] = __builtin_amdgcn_perm(v[2 * j + 1][d >> 3][(d & 7) >> 1], v[2 * j][d >> 3][(d & 7) >> 1], (d & 1) ? 0x07060302u : 0x05040100u);
-      o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), pf, o[d], 0, 0, 0);
+      const bf16x8 wf = __builtin_bit_cast(bf16x8, w);
+      o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, pr, o[d], 0, 0, 0);
+      o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, pu, o[d], 0, 0, 0);
     }
   }
 };

@@ -1,0 +1,40 @@
+"""Decode kernels on calls that the definitions allow and ordinary inputs do not make: infinities, ties under a threshold that no
+weight reaches, rows that begin between 16 bytes, fp32 angles of far positions.
+
+u = 2^-24 (fp32), half a step of bf16 relative to the value 2^-8; tolerances are derived beside their use."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from oracle import zo_decode as od
+from paper_2605_28760_amd import binding as zb
+from test_gpu_decode import DEV, HALF, TT, U, ZT, Setup, _check_draw, _i32, _np
+
+
+def _exact(s, t, head, scale):
+    """(output, sum of weights times |values|, largest scale * |q| |k|) of a row and head in 64 bits."""
+    i, pos = od.row_places(s.cu, s.kv)[t]
+    n = head // (s.H // s.g)
+    at = [(od.page_of(s.table, s.P, s.n_pages, i, j), j % s.P) for j in range(pos + 1)]
+    pg, sl = np.array([x for x in at if x[0] is not None]).T
+    k, v, q = _np(s.K[pg, n, sl]), _np(s.V[pg, n, sl]), _np(s.q[t]).reshape(s.H, s.dh)[head]
+    z = scale * (k @ q)
+    p = np.exp(z - z.max())
+    p /= p.sum()
+    return p @ v, p @ np.abs(v), abs(scale) * (np.abs(k) @ np.abs(q)).max(), len(p)
+
+
+@pytest.mark.parametrize("H,g,dh,kv", [(4, 1, 128, [2, 16, 33, 257, 700]), (20, 1, 64, [5, 300]), (3, 3, 256, [31, 600]), (8, 2, 128, [3000])])
+def test_bf16_attention_rounds_its_output_only(H, g, dh, kv):
+    """The weights keep 15 bits and more (2^-15 + 2^-20 of each): what is left is the fp32 arithmetic, scores (dh + 3) u of
+    scale * sum |q_d k_d| (twice that in the quotient) and n + 16 roundings of the sums, and the output's own half step."""
+    s = Setup(H + dh, "bf16", H, g, dh, 16, [1] * len(kv), kv)
+    out, scale = _np(s.attend()), dh ** -0.5
+    for t in range(s.T):
+        for head in range(H):
+            want, size, big, n = _exact(s, t, head, scale)
+            tol = (2 * (dh + 3) * U * big + (n + 16) * U + 2.0 ** -15 + 2.0 ** -20) * size + 2.0 ** -8 * np.abs(want)
+            err = np.abs(out[t, head * dh:(head + 1) * dh] - want)
+            assert (err <= tol).all(), (t, head, float((err / tol).max()))
