@@ -472,7 +472,8 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
   const float mp = a.min_p ? a.min_p[row] : 0.f;
   const float u0 = a.u[row];
   const double u1 = u0 > 0.f ? (u0 < 1.f ? (double)u0 : 1.0) : 0.0;
-  const bool greedy = !(temp > 0.f);
+  // (no weight reaches a min_p above 1: the first of the order is kept, as without a temperature)
+  const bool greedy = !(temp > 0.f) || mp > 1.f;
   auto answer = [&](int token, double prob, u64 number) __attribute__((always_inline)) {
     a.tokens[row] = token;
     if (a.prob) a.prob[row] = (float)prob;
@@ -536,7 +537,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
   }
   const Scale sc(best, temp);
   auto weight = [&](float x) { return sc.weight(x); };
-  auto by_min = [&](float x, double w) { return w >= min_w || x == sc.zmax; };
+  auto by_min = [&](double w) { return w >= min_w; };   // (the largest weight is exactly 1)
 
   // ---- the tokens of bins 0 .. `to` hold the prefix; n_to of them, about
   int to = kLast;
@@ -681,7 +682,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
       block_scan(s, lane, wave, un, 0.0, nb, mb);
       in = in && (tid == 0 || (double)nb * 0x1p-50 < (double)p * z_k);
     }
-    in = in && by_min(x, w);
+    in = in && by_min(w);
     un = in ? un : 0;
     const u64 sum = block_sum(s, lane, wave, un);
     const u64 number = block_sum(s, lane, wave, (u64)in);
@@ -808,13 +809,13 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
     auto val = [&](float x, int i) __attribute__((always_inline)) -> u64 {
       if (!kept(x, i)) return 0;
       const double w = weight(x);
-      return by_min(x, w) ? Scale::units(w) : 0;
+      return by_min(w) ? Scale::units(w) : 0;
     };
     u64 sum = 0, number = 0;
     each_listed([&](float x, int i) {
       if (!kept(x, i)) return;
       const double w = weight(x);
-      if (!by_min(x, w)) return;
+      if (!by_min(w)) return;
       ++number;
       sum += Scale::units(w);
     });
@@ -857,7 +858,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
     auto add = [&](float z, bool there, double w) __attribute__((always_inline)) {
       bool take = there && z >= sc.far;
       if (limit_m) {
-        take = take && by_min(z, w);
+        take = take && by_min(w);
         number += (unsigned)__popcll(__ballot(take));
       }
       part += take ? w : 0.0;
@@ -927,7 +928,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       w[j] = kept(x[j], first + j) ? weight(x[j]) : 0.0;
-      if (!by_min(x[j], w[j])) w[j] = 0.0;
+      if (!by_min(w[j])) w[j] = 0.0;
       run += w[j];
     }
     const double inc = wave_scan(run);

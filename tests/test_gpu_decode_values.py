@@ -38,3 +38,25 @@ def test_bf16_attention_rounds_its_output_only(H, g, dh, kv):
             tol = (2 * (dh + 3) * U * big + (n + 16) * U + 2.0 ** -15 + 2.0 ** -20) * size + 2.0 ** -8 * np.abs(want)
             err = np.abs(out[t, head * dh:(head + 1) * dh] - want)
             assert (err <= tol).all(), (t, head, float((err / tol).max()))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [2, 300, 3001, 9001])
+def test_min_p_above_one_keeps_the_first_of_the_largest(dtype, V):
+    """No weight reaches it: max(1, 0) tokens are kept, also where several share the maximum."""
+    rng = np.random.default_rng(V)
+    z = np.round(rng.normal(size=(8, V)))
+    z[0] = 0.25
+    z[1, V // 2:] = z[1].max() + 1
+    z[2, [0, V - 1]] = np.inf
+    z[3] = np.inf
+    z[4, ::2] = -np.inf
+    z[5] = -np.inf
+    z[6, V // 3:] = np.nan
+    zt = torch.from_numpy(z).to(DEV).to(TT[dtype])
+    u = [0.9, 0.9, 0.9, 0.5, 0.9, 0.9, 0.9, 1.0]
+    for m in (1.5, float(np.nextafter(np.float32(1), np.float32(2))), np.inf):
+        for k, p in ((None, None), ([V - 1] * 8, None), (None, [0.999] * 8), ([200] * 8, [0.999] * 8)):
+            _check_draw(zt, [0.7] * 8, k, p, [m] * 8, u)
+    _check_draw(zt, [0.7] * 8, None, None, [1.0] * 8, u)        # (the weight at the maximum reaches 1)
+    _check_draw(zt, [0.7] * 8, None, None, [1.5, 1.0] * 4, u)   # rows of both kinds
