@@ -173,6 +173,14 @@ __device__ __forceinline__ T of_lane(T v, int lane) { return __shfl(v, lane); }
 template <class T>
 __device__ __forceinline__ T wave_sum(T v) { return of_lane(wave_scan(v), kWave - 1); }
 
+// Between LDS accesses of the wave's own lanes to each other's places: a wave's accesses are executed in order, and this keeps the
+// compiler from exchanging them.
+__device__ __forceinline__ void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 struct Shared {
   uint32_t cnt[kBins];
   u64 mass[kBins];
@@ -886,10 +894,12 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
           if (in[u][j]) packed[at + __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0))] = x[u][j];
           at += __popcll(m);
         }
+      wave_lds_order();
       for (int e = 0; e < n; e += kWave) {
         const float z = e + lane < n ? packed[e + lane] : sc.zmax;
         add(z, e + lane < n, exp2_neg(sc.diff(z), sc.c));
       }
+      wave_lds_order();   // (the next strip's come to the same place)
     }
     const double sum = wave_sum(part);
     if (lane == 0) s.strip[st] = sum;
