@@ -484,9 +484,9 @@ int32_t zo_cache_append(const zo_batch* batch, const void* Q, int64_t ldq, const
  * Attention of new rows over the cache (their own keys and values stored by zo_cache_append first):
  *   O[t, h] = sum_j softmax_j(scale * <Q[t, h], K[j, g]>) V[j, g],   g = h / (n_heads / n_kv_heads),
  *   j over the positions 0 .. pos(t) of the row's sequence
- * A row that sees no position (kv_len 0, or only pages outside the pool) gets zeros; rows behind the last
- * sequence are left as they were.  O must not overlap Q or the pools.  Laid out for one row per sequence; several rows of
- * a sequence each read its cache.
+ * A row that sees no position (kv_len 0, or only pages outside the pool) gets zeros; one that sees positions, but whose scores
+ * are all -infinity, has no softmax and gets NaN.  Rows behind the last sequence are left as they were.  O must not overlap Q or
+ * the pools.  Laid out for one row per sequence; several rows of a sequence each read its cache.
  * ZO_BF16: head_dim 64, 128 or 256; products on bf16 MFMA with fp32 accumulation, softmax in fp32, weights
  * as the sum of two bf16 values in the second product (2^-15 of a weight is lost at most).  ZO_F32: head_dim <= 256,
  * fp32 throughout.

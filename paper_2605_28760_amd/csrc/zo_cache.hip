@@ -431,6 +431,13 @@ struct Joined {
   f32x4 o;
 };
 
+// The maximum of a query that has met keys, but none above -infinity: beside a larger one it has no weight, alone it has no softmax.
+constexpr float kLeast = -3.402823466e38f;
+// What the output is multiplied by: zeros stay zeros where no key was met.
+__device__ __forceinline__ float inverse_sum(float m, float l) {
+  return l > 0.f ? 1.0f / l : m == -INFINITY ? 0.f : __builtin_nanf("");
+}
+
 // kTiles: tiles of 16 query heads per workgroup (1 or 2); with one its waves share the keys.  kRanges: ranges of a row per
 // workgroup, 1 or kHere (then the table has room for no more).
 template <typename Tio, class Step, int kTiles, int kRanges>
@@ -465,6 +472,7 @@ __global__ __launch_bounds__(kRanges* kRangeWaves* kWave, Step::kPad > 128 ? 1 :
 #pragma unroll
     for (int d = 0; d < kCols; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;   // l: this lane's share
+    bool met = false;               // a key that is seen
 
     // pages of the 64 blocks of 16 positions that begin at block `first`, one a lane; -1: no position, or no page of the pool
     auto pages_from = [&](int first) {
@@ -501,6 +509,7 @@ __global__ __launch_bounds__(kRanges* kRangeWaves* kWave, Step::kPad > 128 ? 1 :
       return true;
     };
     auto attend = [&](const Step& st, int last, int dead) {
+      met = true;
       float s[Step::kScores];
       st.scores(q, s);
 #pragma unroll
@@ -558,6 +567,7 @@ __global__ __launch_bounds__(kRanges* kRangeWaves* kWave, Step::kPad > 128 ? 1 :
     // ---- the waves join
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
+    if (met) m = fmaxf(m, kLeast);
     if (r < cols) {
       float* row = s_o + (wave * 16 + r) * kRowLds + g * (kDh / 4);   // columns (4 g + i) kCols + d
 #pragma unroll
@@ -612,7 +622,7 @@ __global__ __launch_bounds__(kRanges* kRangeWaves* kWave, Step::kPad > 128 ? 1 :
         x.l = (lf[0] + lf[2]) + (lf[1] + lf[3]);   // (the order of the wave's sum)
       }
       if (kRanges > 1 || n_ranges == 1) {
-        const float inv = x.l > 0.f ? 1.0f / x.l : x.l;   // (NaN stays NaN)
+        const float inv = inverse_sum(x.m, x.l);
         Tio* out = (Tio*)a.O + (int64_t)t * a.ldo + (int64_t)h * a.c.dh + d;
         if constexpr (sizeof(Tio) == 2) {
           *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(x.o[0] * inv, x.o[1] * inv), pack_bf16x2(x.o[2] * inv, x.o[3] * inv));
@@ -713,7 +723,7 @@ __global__ __launch_bounds__(kJoinSums* kWave) void k_attention_join(PagedAttnAr
       for (int i = 0; i < kPer; ++i) acc[0][i] += s_acc[v - 1][i * kWave + lane];
   }
   const float sum = wave_sum(l * f);
-  const float inv = sum > 0.f ? 1.0f / sum : sum;
+  const float inv = inverse_sum(mm, sum);
 #pragma unroll
   for (int i = 0; i < kPer; ++i)
     if (lane + i * kWave < dh) st_elem((Tio*)a.O + (int64_t)t * a.ldo + (int64_t)h * dh, lane + i * kWave, acc[0][i] * inv);

@@ -60,3 +60,24 @@ def test_min_p_above_one_keeps_the_first_of_the_largest(dtype, V):
             _check_draw(zt, [0.7] * 8, k, p, [m] * 8, u)
     _check_draw(zt, [0.7] * 8, None, None, [1.0] * 8, u)        # (the weight at the maximum reaches 1)
     _check_draw(zt, [0.7] * 8, None, None, [1.5, 1.0] * 4, u)   # rows of both kinds
+
+
+@pytest.mark.parametrize("dtype,dh", [("bf16", 128), ("bf16", 64), ("bf16", 256), ("f32", 64), ("f32", 128), ("f32", 24)])
+@pytest.mark.parametrize("width", [64, 200])
+def test_a_query_whose_scores_are_all_minus_infinity(dtype, dh, width):
+    """Its softmax has no value: NaN, in whichever way the ranges are joined.  A range of them beside a finite one has no weight;
+    a row that sees no position stays zero."""
+    kv = [1, 45, 300, 700, 900, 0, 900]
+    s = Setup(31, dtype, 4, 2, dh, 16, [1] * len(kv), kv, width=width)
+    s.q[:, 0::dh] = s.q[:, 0::dh].abs() + 0.1
+    for i, n in enumerate((1, 45, 300, 700, 640, 0, 0)):
+        for p in range(n):
+            s.K[int(s.table[i, p // 16]), :, p % 16, 0] = float("-inf")
+    s.table[6] = -1
+    s.d_table.copy_(_i32(s.table))
+    got = _np(s.attend())[:, :4 * dh]
+    assert np.isnan(got[:4]).all()
+    assert (got[5:] == 0).all()
+    s.kv[0:4] = [0] * 4
+    got[:4] = 0
+    s.check_attend(torch.from_numpy(got))
