@@ -465,189 +465,186 @@ __global__ __launch_bounds__(kRanges* kRangeWaves* kWave, Step::kPad > 128 ? 1 :
   const float sl2 = a.scale * 1.4426950408889634f;           // scores are kept in base-2 units
   const int32_t* table = a.c.table + (int64_t)pl.seq * a.c.max_pages;
 
-  for (int range0 = blockIdx.y; range0 < n_ranges; range0 += gridDim.y) {
-    const int range = kRanges == 1 ? range0 : wave / kRangeWaves;
-    const int j_a = range * len, j_b = min(j_a + len, n);   // the range's positions (none behind the row's last)
-    f32x4 o[kCols];
+  if ((int)blockIdx.y >= n_ranges) return;   // (the grid has the ranges of the longest row that the table has room for)
+  const int range = kRanges == 1 ? (int)blockIdx.y : wave / kRangeWaves;
+  const int j_a = range * len, j_b = min(j_a + len, n);   // the range's positions (none behind the row's last)
+  f32x4 o[kCols];
 #pragma unroll
-    for (int d = 0; d < kCols; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, l = 0.f;   // l: this lane's share
-    bool met = false;               // a key that is seen
+  for (int d = 0; d < kCols; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;   // l: this lane's share
+  bool met = false;               // a key that is seen
 
-    // pages of the 64 blocks of 16 positions that begin at block `first`, one a lane; -1: no position, or no page of the pool
-    auto pages_from = [&](int first) {
-      const int j = (first + lane) * 16;
-      if (j >= j_b) return -1;
-      const int pg = table[j >> a.c.page_shift];
-      return (unsigned)pg < (unsigned)a.c.n_pages ? pg : -1;
-    };
-    int first = j_a / 16;
-    int pages = pages_from(first);
-    // Loads step `j0`; false when it has no key that is seen.  A key that is not seen is stood in for by one that is: what a
-    // slot behind the last position holds must not meet even a weight of zero.
-    auto load = [&](int j0, Step& st, int& last, int& dead) -> bool {
-      if (j0 / 16 - first >= 64) {
-        first += 64;
-        pages = pages_from(first);
+  // pages of the 64 blocks of 16 positions that begin at block `first`, one a lane; -1: no position, or no page of the pool
+  auto pages_from = [&](int first) {
+    const int j = (first + lane) * 16;
+    if (j >= j_b) return -1;
+    const int pg = table[j >> a.c.page_shift];
+    return (unsigned)pg < (unsigned)a.c.n_pages ? pg : -1;
+  };
+  int first = j_a / 16;
+  int pages = pages_from(first);
+  // Loads step `j0`; false when it has no key that is seen.  A key that is not seen is stood in for by one that is: what a
+  // slot behind the last position holds must not meet even a weight of zero.
+  auto load = [&](int j0, Step& st, int& last, int& dead) -> bool {
+    if (j0 / 16 - first >= 64) {
+      first += 64;
+      pages = pages_from(first);
+    }
+    const int b = j0 / 16 - first;
+    const int p0 = __builtin_amdgcn_readlane(pages, b);
+    const int p1 = kKeys == 32 ? __builtin_amdgcn_readlane(pages, b + 1) : p0;
+    dead = (p0 < 0 ? 1 : 0) | (p1 < 0 ? 2 : 0);
+    if (p0 < 0 && p1 < 0) return false;
+    last = j_b - 1 - j0;
+    const int64_t b0 = slot_at(a.c, p0 < 0 ? p1 : p0, kvh, j0), b1 = slot_at(a.c, p1 < 0 ? p0 : p1, kvh, j0 + 16);
+    const bool whole = dead == 0 && last >= kKeys - 1;
+    st.load(a, r, g, [&](int key) -> int64_t {
+      int e = key;
+      if (!whole) {
+        if (kKeys == 32 && (dead >> (key >> 4) & 1)) e ^= 16;
+        e = min(e, last);
       }
-      const int b = j0 / 16 - first;
-      const int p0 = __builtin_amdgcn_readlane(pages, b);
-      const int p1 = kKeys == 32 ? __builtin_amdgcn_readlane(pages, b + 1) : p0;
-      dead = (p0 < 0 ? 1 : 0) | (p1 < 0 ? 2 : 0);
-      if (p0 < 0 && p1 < 0) return false;
-      last = j_b - 1 - j0;
-      const int64_t b0 = slot_at(a.c, p0 < 0 ? p1 : p0, kvh, j0), b1 = slot_at(a.c, p1 < 0 ? p0 : p1, kvh, j0 + 16);
-      const bool whole = dead == 0 && last >= kKeys - 1;
-      st.load(a, r, g, [&](int key) -> int64_t {
-        int e = key;
-        if (!whole) {
-          if (kKeys == 32 && (dead >> (key >> 4) & 1)) e ^= 16;
-          e = min(e, last);
-        }
-        return (kKeys == 32 && e >= 16 ? b1 : b0) + (e & 15) * a.c.dh;
-      });
-      return true;
-    };
-    auto attend = [&](const Step& st, int last, int dead) {
-      met = true;
-      float s[Step::kScores];
-      st.scores(q, s);
+      return (kKeys == 32 && e >= 16 ? b1 : b0) + (e & 15) * a.c.dh;
+    });
+    return true;
+  };
+  auto attend = [&](const Step& st, int last, int dead) {
+    met = true;
+    float s[Step::kScores];
+    st.scores(q, s);
 #pragma unroll
-      for (int i = 0; i < Step::kScores; ++i) s[i] *= sl2;
-      if (dead != 0 || last < kKeys - 1) {
-#pragma unroll
-        for (int i = 0; i < Step::kScores; ++i) {
-          const int key = Step::key_of_score(g, i);
-          if (key > last || (dead >> (key >> 4) & 1)) s[i] = -INFINITY;
-        }
-      }
-      float mx = s[0];
-#pragma unroll
-      for (int i = 1; i < Step::kScores; ++i) mx = fmaxf(mx, s[i]);
-      float f = 1.0f;
-      if (__any(mx > m)) {   // (otherwise every factor is one)
-        const float m2 = fmaxf(column_max(mx), m);
-        f = m == m2 ? 1.0f : __builtin_amdgcn_exp2f(m - m2);   // (a query that has met nothing above -infinity yet stays as it is)
-        m = m2;
-#pragma unroll
-        for (int d = 0; d < kCols; ++d) o[d] *= f;
-      }
-      float p[Step::kScores], sum = 0.f;
-      const float off = m == -INFINITY ? 0.f : m;
+    for (int i = 0; i < Step::kScores; ++i) s[i] *= sl2;
+    if (dead != 0 || last < kKeys - 1) {
 #pragma unroll
       for (int i = 0; i < Step::kScores; ++i) {
-        p[i] = __builtin_amdgcn_exp2f(s[i] - off);
-        sum += p[i];
-      }
-      l = __builtin_fmaf(l, f, sum);
-      st.values(p, o);
-    };
-    if (cols > 0) {
-      constexpr int kStride = kSharers * kKeys;
-      int j0 = j_a + share * kKeys;
-      if constexpr (Step::kAhead) {   // two steps in registers: while one is worked on, the next is on its way
-        Step s0, s1;
-        int last0 = 0, dead0 = 0, last1 = 0, dead1 = 0;
-        bool seen0 = j0 < j_b && load(j0, s0, last0, dead0);
-        for (; j0 < j_b; j0 += 2 * kStride) {
-          const bool seen1 = j0 + kStride < j_b && load(j0 + kStride, s1, last1, dead1);
-          if (seen0) attend(s0, last0, dead0);
-          seen0 = j0 + 2 * kStride < j_b && load(j0 + 2 * kStride, s0, last0, dead0);
-          if (seen1) attend(s1, last1, dead1);
-        }
-      } else {
-        for (; j0 < j_b; j0 += kStride) {
-          Step st;
-          int last, dead;
-          if (load(j0, st, last, dead)) attend(st, last, dead);
-        }
+        const int key = Step::key_of_score(g, i);
+        if (key > last || (dead >> (key >> 4) & 1)) s[i] = -INFINITY;
       }
     }
+    float mx = s[0];
+#pragma unroll
+    for (int i = 1; i < Step::kScores; ++i) mx = fmaxf(mx, s[i]);
+    float f = 1.0f;
+    if (__any(mx > m)) {   // (otherwise every factor is one)
+      const float m2 = fmaxf(column_max(mx), m);
+      f = m == m2 ? 1.0f : __builtin_amdgcn_exp2f(m - m2);   // (a query that has met nothing above -infinity yet stays as it is)
+      m = m2;
+#pragma unroll
+      for (int d = 0; d < kCols; ++d) o[d] *= f;
+    }
+    float p[Step::kScores], sum = 0.f;
+    const float off = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int i = 0; i < Step::kScores; ++i) {
+      p[i] = __builtin_amdgcn_exp2f(s[i] - off);
+      sum += p[i];
+    }
+    l = __builtin_fmaf(l, f, sum);
+    st.values(p, o);
+  };
+  if (cols > 0) {
+    constexpr int kStride = kSharers * kKeys;
+    int j0 = j_a + share * kKeys;
+    if constexpr (Step::kAhead) {   // two steps in registers: while one is worked on, the next is on its way
+      Step s0, s1;
+      int last0 = 0, dead0 = 0, last1 = 0, dead1 = 0;
+      bool seen0 = j0 < j_b && load(j0, s0, last0, dead0);
+      for (; j0 < j_b; j0 += 2 * kStride) {
+        const bool seen1 = j0 + kStride < j_b && load(j0 + kStride, s1, last1, dead1);
+        if (seen0) attend(s0, last0, dead0);
+        seen0 = j0 + 2 * kStride < j_b && load(j0 + 2 * kStride, s0, last0, dead0);
+        if (seen1) attend(s1, last1, dead1);
+      }
+    } else {
+      for (; j0 < j_b; j0 += kStride) {
+        Step st;
+        int last, dead;
+        if (load(j0, st, last, dead)) attend(st, last, dead);
+      }
+    }
+  }
 
-    // ---- the waves join
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
-    if (met) m = fmaxf(m, kLeast);
-    if (r < cols) {
-      float* row = s_o + (wave * 16 + r) * kRowLds + g * (kDh / 4);   // columns (4 g + i) kCols + d
+  // ---- the waves join
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+  if (met) m = fmaxf(m, kLeast);
+  if (r < cols) {
+    float* row = s_o + (wave * 16 + r) * kRowLds + g * (kDh / 4);   // columns (4 g + i) kCols + d
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int d = 0; d < kCols; d += 4)
-          *reinterpret_cast<f32x4*>(row + i * kCols + d) = f32x4{o[d][i], o[d + 1][i], o[d + 2][i], o[d + 3][i]};
-      if (g == 0) { s_m[wave][r] = m; s_l[wave][r] = l; }
-    }
-    __syncthreads();
-    const int group_cols = min(16 * kTiles, a.group - part * 16 * kTiles);
-    for (int e = threadIdx.x; e < group_cols * (kDh / 4); e += kAttnWaves * kWave) {
-      const int c = e / (kDh / 4), col = c & 15, tl = c >> 4, d = e % (kDh / 4) * 4;
-      auto waves_of = [&](int rg) {   // the waves of one range
-        Joined x{-INFINITY, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
+      for (int d = 0; d < kCols; d += 4)
+        *reinterpret_cast<f32x4*>(row + i * kCols + d) = f32x4{o[d][i], o[d + 1][i], o[d + 2][i], o[d + 3][i]};
+    if (g == 0) { s_m[wave][r] = m; s_l[wave][r] = l; }
+  }
+  __syncthreads();
+  const int group_cols = min(16 * kTiles, a.group - part * 16 * kTiles);
+  for (int e = threadIdx.x; e < group_cols * (kDh / 4); e += kAttnWaves * kWave) {
+    const int c = e / (kDh / 4), col = c & 15, tl = c >> 4, d = e % (kDh / 4) * 4;
+    auto waves_of = [&](int rg) {   // the waves of one range
+      Joined x{-INFINITY, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-        for (int w = 0; w < kSharers; ++w) x.m = fmaxf(x.m, s_m[rg * kRangeWaves + w * kTiles + tl][col]);
+      for (int w = 0; w < kSharers; ++w) x.m = fmaxf(x.m, s_m[rg * kRangeWaves + w * kTiles + tl][col]);
 #pragma unroll
-        for (int w = 0; w < kSharers; ++w) {
-          const int wv = rg * kRangeWaves + w * kTiles + tl;
-          const float mw = s_m[wv][col];
-          const float f = mw == x.m ? 1.0f : __builtin_amdgcn_exp2f(mw - x.m);   // (no key at all: zeros stay zeros)
-          const f32x4 ow = *reinterpret_cast<const f32x4*>(s_o + (wv * 16 + col) * kRowLds + d);
+      for (int w = 0; w < kSharers; ++w) {
+        const int wv = rg * kRangeWaves + w * kTiles + tl;
+        const float mw = s_m[wv][col];
+        const float f = mw == x.m ? 1.0f : __builtin_amdgcn_exp2f(mw - x.m);   // (no key at all: zeros stay zeros)
+        const f32x4 ow = *reinterpret_cast<const f32x4*>(s_o + (wv * 16 + col) * kRowLds + d);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x.o[i] = __builtin_fmaf(ow[i], f, x.o[i]);
-          x.l = __builtin_fmaf(s_l[wv][col], f, x.l);
-        }
-        return x;
-      };
-      const int h = kvh * a.group + part * 16 * kTiles + c;
-      Joined x;
-      if (kRanges == 1 || n_ranges == 1) {
-        x = waves_of(0);
-      } else {   // what k_attention_join does, for four ranges
+        for (int i = 0; i < 4; ++i) x.o[i] = __builtin_fmaf(ow[i], f, x.o[i]);
+        x.l = __builtin_fmaf(s_l[wv][col], f, x.l);
+      }
+      return x;
+    };
+    const int h = kvh * a.group + part * 16 * kTiles + c;
+    Joined x;
+    if (kRanges == 1 || n_ranges == 1) {
+      x = waves_of(0);
+    } else {   // what k_attention_join does, for four ranges
 #pragma clang fp contract(off)
-        Joined y[kHere];
-        x = Joined{-INFINITY, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
+      Joined y[kHere];
+      x = Joined{-INFINITY, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-        for (int rg = 0; rg < kHere; ++rg) {
-          y[rg] = Joined{-INFINITY, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
-          if (rg < n_ranges) y[rg] = waves_of(rg);
-          x.m = fmaxf(x.m, y[rg].m);
-        }
-        float lf[kHere];
-#pragma unroll
-        for (int rg = 0; rg < kHere; ++rg) {
-          const float f = y[rg].m == x.m ? 1.0f : __builtin_amdgcn_exp2f(y[rg].m - x.m);
-          lf[rg] = y[rg].l * f;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) x.o[i] = x.o[i] + y[rg].o[i] * f;
-        }
-        x.l = (lf[0] + lf[2]) + (lf[1] + lf[3]);   // (the order of the wave's sum)
+      for (int rg = 0; rg < kHere; ++rg) {
+        y[rg] = Joined{-INFINITY, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
+        if (rg < n_ranges) y[rg] = waves_of(rg);
+        x.m = fmaxf(x.m, y[rg].m);
       }
-      if (kRanges > 1 || n_ranges == 1) {
-        const float inv = inverse_sum(x.m, x.l);
-        Tio* out = (Tio*)a.O + (int64_t)t * a.ldo + (int64_t)h * a.c.dh + d;
-        if constexpr (sizeof(Tio) == 2) {
-          *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(x.o[0] * inv, x.o[1] * inv), pack_bf16x2(x.o[2] * inv, x.o[3] * inv));
-        } else if constexpr (Step::kWhole) {
-          *reinterpret_cast<f32x4*>(out) = x.o * inv;
-        } else {
+      float lf[kHere];
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (d + i < a.c.dh) out[i] = x.o[i] * inv;
-        }
+      for (int rg = 0; rg < kHere; ++rg) {
+        const float f = y[rg].m == x.m ? 1.0f : __builtin_amdgcn_exp2f(y[rg].m - x.m);
+        lf[rg] = y[rg].l * f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x.o[i] = x.o[i] + y[rg].o[i] * f;
+      }
+      x.l = (lf[0] + lf[2]) + (lf[1] + lf[3]);   // (the order of the wave's sum)
+    }
+    if (kRanges > 1 || n_ranges == 1) {
+      const float inv = inverse_sum(x.m, x.l);
+      Tio* out = (Tio*)a.O + (int64_t)t * a.ldo + (int64_t)h * a.c.dh + d;
+      if constexpr (sizeof(Tio) == 2) {
+        *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(x.o[0] * inv, x.o[1] * inv), pack_bf16x2(x.o[2] * inv, x.o[3] * inv));
+      } else if constexpr (Step::kWhole) {
+        *reinterpret_cast<f32x4*>(out) = x.o * inv;
       } else {
-        const int64_t at = part_at(a, t, h, range);
-        if (d == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = make_float2(x.m, x.l);
-        float* out = a.part_o + at * a.c.dh + d;
-        if constexpr (Step::kWhole) {
-          *reinterpret_cast<f32x4*>(out) = x.o;
-        } else {
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (d + i < a.c.dh) out[i] = x.o[i];
-        }
+        for (int i = 0; i < 4; ++i)
+          if (d + i < a.c.dh) out[i] = x.o[i] * inv;
+      }
+    } else {
+      const int64_t at = part_at(a, t, h, range);
+      if (d == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = make_float2(x.m, x.l);
+      float* out = a.part_o + at * a.c.dh + d;
+      if constexpr (Step::kWhole) {
+        *reinterpret_cast<f32x4*>(out) = x.o;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (d + i < a.c.dh) out[i] = x.o[i];
       }
     }
-    if (kRanges > 1) break;
-    if (range0 + (int)gridDim.y < n_ranges) __syncthreads();   // (the buffer is written again)
   }
 }
 

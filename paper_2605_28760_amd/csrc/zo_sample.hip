@@ -193,7 +193,7 @@ struct Shared {
   double wave_m[kWaves];
   float wave_z[kWaves];
   // results of one thread, for all
-  uint32_t lo, hi, n_list;
+  uint32_t lo, n_list;
   int bin, index;
   u64 n_before, n_at;
   double m_before, m_at, total;
