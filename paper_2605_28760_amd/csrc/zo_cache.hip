@@ -292,8 +292,10 @@ __device__ __forceinline__ int64_t part_at(const PagedAttnArgs& a, int t, int h,
   return ((int64_t)t * a.n_heads + h) * a.ranges + range;
 }
 
+__device__ __attribute__((aligned(16))) const uint32_t kZeros[256] = {};   // the value of a key that is not seen
+
 // What differs between the two types: loading a step's keys and values and the two products.
-// eff(key): which of the step's keys stands in for `key`; at(key): its first element in the pools.
+// at(key), value_at(key): the first element of what is read for a key of the step and for its value, in the pools.
 template <int kDh>
 struct Bf16Step {
   static constexpr int kKeys = 32, kPad = kDh, kCols = kDh / 16;   // columns of a value row per lane
@@ -303,8 +305,8 @@ struct Bf16Step {
   u32x4 v[8][kCols > 8 ? kCols / 8 : 1];  // (kCols 4: the lower half of each)
   __device__ static constexpr int key_of_score(int g, int i) { return 8 * g + i; }
 
-  template <class At>
-  __device__ __forceinline__ void load(const PagedAttnArgs& a, int r, int g, At at) {
+  template <class At, class ValueAt>
+  __device__ __forceinline__ void load(const PagedAttnArgs& a, int r, int g, At at, ValueAt value_at) {
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf) {
       const bf16_t* p = (const bf16_t*)a.c.K + at(8 * (r >> 2) + (r & 3) + 4 * hf) + g * 8;
@@ -313,7 +315,7 @@ struct Bf16Step {
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const bf16_t* p = (const bf16_t*)a.c.V + at(8 * g + j) + r * kCols;
+      const bf16_t* p = (const bf16_t*)a.c.V + value_at(8 * g + j) + r * kCols;
       if constexpr (kCols == 4) {
         const uint2 w = *reinterpret_cast<const uint2*>(p);
         v[j][0] = u32x4{w.x, w.y, 0u, 0u};
@@ -388,14 +390,14 @@ struct F32Step {
     }
     return x;
   }
-  template <class At>
-  __device__ __forceinline__ void load(const PagedAttnArgs& a, int r, int g, At at) {
+  template <class At, class ValueAt>
+  __device__ __forceinline__ void load(const PagedAttnArgs& a, int r, int g, At at, ValueAt value_at) {
     const float* p = (const float*)a.c.K + at(r);
 #pragma unroll
     for (int ks = 0; ks < kDh / 16; ++ks) k[ks] = four(p, ks * 16 + g * 4, a.c.dh);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float* w = (const float*)a.c.V + at(4 * g + j);
+      const float* w = (const float*)a.c.V + value_at(4 * g + j);
 #pragma unroll
       for (int c = 0; c < kCols / 4; ++c) v[j][c] = four(w, r * kCols + c * 4, a.c.dh);
     }
@@ -464,6 +466,8 @@ __global__ __launch_bounds__(kRanges* kRangeWaves* kWave, Step::kPad > 128 ? 1 :
   Step::load_query(a, (const Tio*)a.Q + (int64_t)t * a.ldq + (int64_t)(kvh * a.group + head0 + r) * a.c.dh, r < cols, g, q);
   const float sl2 = a.scale * 1.4426950408889634f;           // scores are kept in base-2 units
   const int32_t* table = a.c.table + (int64_t)pl.seq * a.c.max_pages;
+  // the zeros' place as an element of the pool of values (both lie on 16 bytes)
+  const int64_t no_value = ((int64_t)(uintptr_t)kZeros - (int64_t)(uintptr_t)a.c.V) / (int64_t)sizeof(Tio);
 
   if ((int)blockIdx.y >= n_ranges) return;   // (the grid has the ranges of the longest row that the table has room for)
   const int range = kRanges == 1 ? (int)blockIdx.y : wave / kRangeWaves;
@@ -483,8 +487,9 @@ __global__ __launch_bounds__(kRanges* kRangeWaves* kWave, Step::kPad > 128 ? 1 :
   };
   int first = j_a / 16;
   int pages = pages_from(first);
-  // Loads step `j0`; false when it has no key that is seen.  A key that is not seen is stood in for by one that is: what a
-  // slot behind the last position holds must not meet even a weight of zero.
+  // Loads step `j0`; false when it has no key that is seen.  A key that is not seen is stood in for by one that is (its score is
+  // replaced below), its value by zeros: what a slot holds that is not seen, and an infinite value of the stand-in's, must not
+  // meet even a weight of zero.
   auto load = [&](int j0, Step& st, int& last, int& dead) -> bool {
     if (j0 / 16 - first >= 64) {
       first += 64;
@@ -498,14 +503,17 @@ __global__ __launch_bounds__(kRanges* kRangeWaves* kWave, Step::kPad > 128 ? 1 :
     last = j_b - 1 - j0;
     const int64_t b0 = slot_at(a.c, p0 < 0 ? p1 : p0, kvh, j0), b1 = slot_at(a.c, p1 < 0 ? p0 : p1, kvh, j0 + 16);
     const bool whole = dead == 0 && last >= kKeys - 1;
-    st.load(a, r, g, [&](int key) -> int64_t {
+    auto seen = [&](int key) { return key <= last && !(dead >> (key >> 4) & 1); };
+    auto at = [&](int key) -> int64_t {
       int e = key;
       if (!whole) {
         if (kKeys == 32 && (dead >> (key >> 4) & 1)) e ^= 16;
         e = min(e, last);
       }
       return (kKeys == 32 && e >= 16 ? b1 : b0) + (e & 15) * a.c.dh;
-    });
+    };
+    auto value_at = [&](int key) -> int64_t { return whole || seen(key) ? at(key) : no_value; };
+    st.load(a, r, g, at, value_at);
     return true;
   };
   auto attend = [&](const Step& st, int last, int dead) {
@@ -518,7 +526,7 @@ __global__ __launch_bounds__(kRanges* kRangeWaves* kWave, Step::kPad > 128 ? 1 :
 #pragma unroll
       for (int i = 0; i < Step::kScores; ++i) {
         const int key = Step::key_of_score(g, i);
-        if (key > last || (dead >> (key >> 4) & 1)) s[i] = -INFINITY;
+        if (key > last || (dead >> (key >> 4) & 1)) s[i] = -INFINITY;   // (not seen)
       }
     }
     float mx = s[0];

@@ -81,3 +81,16 @@ def test_a_query_whose_scores_are_all_minus_infinity(dtype, dh, width):
     s.kv[0:4] = [0] * 4
     got[:4] = 0
     s.check_attend(torch.from_numpy(got))
+
+
+@pytest.mark.parametrize("dtype,dh", [("bf16", 128), ("bf16", 64), ("bf16", 256), ("f32", 64), ("f32", 128), ("f32", 24)])
+def test_infinite_values_that_are_seen_stay_infinite(dtype, dh):
+    """The last position's value is infinite and its key stands in for the slots behind it, which have no weight."""
+    kv = [1, 2, 17, 33, 45, 260, 700]
+    s = Setup(32, dtype, 4, 2, dh, 16, [1] * len(kv), kv)
+    for i, n in enumerate(kv):
+        s.V[int(s.table[i, (n - 1) // 16]), :, (n - 1) % 16, 1] = float("inf")
+        s.V[int(s.table[i, (n - 1) // 16]), :, (n - 1) % 16, 2] = float("-inf")
+    got = _np(s.attend())[:, :4 * dh].reshape(len(kv), 4, dh)
+    assert (got[:, :, 1] == np.inf).all() and (got[:, :, 2] == -np.inf).all()
+    assert np.isfinite(got[:, :, 3:]).all()
