@@ -366,6 +366,9 @@ struct Bf16Step {
   }
 };
 
+// Four values of a query or output row, which need no alignment beyond their type's: one access all the same.
+typedef f32x4 __attribute__((aligned(4))) f32x4_any;
+
 // kMode 0: the head dimension is kDh; 1: smaller, a multiple of 4; 2: smaller, any.
 template <int kDh, int kMode>
 struct F32Step {
@@ -377,12 +380,13 @@ struct F32Step {
   f32x4 v[4][kCols / 4];
   __device__ static constexpr int key_of_score(int g, int i) { return 4 * g + i; }
 
-  // four values from column `col` of a row of dh; zeros behind its end
+  // four values from column `col` of a row of dh; zeros behind its end.  F4: as the row is aligned (the pools on 16 bytes)
+  template <class F4 = f32x4>
   __device__ static __forceinline__ f32x4 four(const float* row, int col, int dh) {
-    if constexpr (kMode == 0) return *reinterpret_cast<const f32x4*>(row + col);
+    if constexpr (kMode == 0) return *reinterpret_cast<const F4*>(row + col);
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
     if constexpr (kMode == 1) {
-      if (col < dh) x = *reinterpret_cast<const f32x4*>(row + col);
+      if (col < dh) x = *reinterpret_cast<const F4*>(row + col);
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
@@ -407,7 +411,7 @@ struct F32Step {
 #pragma unroll
     for (int ks = 0; ks < kDh / 16; ++ks) {
       q[ks] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (valid) q[ks] = kMode == 0 ? *reinterpret_cast<const f32x4*>((const float*)row + ks * 16 + g * 4) : four((const float*)row, ks * 16 + g * 4, a.c.dh);
+      if (valid) q[ks] = four<f32x4_any>((const float*)row, ks * 16 + g * 4, a.c.dh);
     }
   }
   __device__ __forceinline__ void scores(const Query& q, float (&s)[kScores]) const {
@@ -635,7 +639,7 @@ __global__ __launch_bounds__(kRanges* kRangeWaves* kWave, Step::kPad > 128 ? 1 :
       if constexpr (sizeof(Tio) == 2) {
         *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(x.o[0] * inv, x.o[1] * inv), pack_bf16x2(x.o[2] * inv, x.o[3] * inv));
       } else if constexpr (Step::kWhole) {
-        *reinterpret_cast<f32x4*>(out) = x.o * inv;
+        *reinterpret_cast<f32x4_any*>(out) = x.o * inv;
       } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)

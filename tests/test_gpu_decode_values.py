@@ -94,3 +94,17 @@ def test_infinite_values_that_are_seen_stay_infinite(dtype, dh):
     got = _np(s.attend())[:, :4 * dh].reshape(len(kv), 4, dh)
     assert (got[:, :, 1] == np.inf).all() and (got[:, :, 2] == -np.inf).all()
     assert np.isfinite(got[:, :, 3:]).all()
+
+
+@pytest.mark.parametrize("dh", [64, 80, 128, 256, 7])
+@pytest.mark.parametrize("offset,pad", [(1, 0), (2, 3), (3, 1), (0, 1)])
+def test_fp32_attention_rows_that_begin_between_16_bytes(dh, offset, pad):
+    kv = [1, 40, 300, 600]
+    s = Setup(33, "f32", 4, 2, dh, 16, [1] * 4, kv)
+    plain = s.attend().clone()[:, :4 * dh]
+    ld = 4 * dh + pad
+    q, o = (torch.full((4 * ld + 8,), 7.0, device=DEV)[offset:offset + 4 * ld].view(4, ld) for _ in range(2))
+    q[:, :4 * dh] = s.q
+    ws = s.workspace()
+    zb.zo_attention_paged(s.batch, q, ld, 4, dh ** -0.5, s.cache, o, ld, ws[0], ws[1])
+    assert torch.equal(o[:, :4 * dh], plain) and (o[:, 4 * dh:] == 7).all()
