@@ -202,7 +202,7 @@ __global__ __launch_bounds__(256) void k_cache_append_heads(AppendArgs a, int pe
     const Place pl = place_of_row(a.cu, a.c.kv_len, a.S, t, lane);
     if (pl.seq < 0) continue;
     const int page = page_of(a.c, pl.seq, pl.pos);
-    float cs[4] = {1.f, 1.f, 1.f, 1.f}, sn[4] = {0.f, 0.f, 0.f, 0.f};
+    float cs[4], sn[4];
     if (a.theta > 0.f) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -231,11 +231,13 @@ __global__ __launch_bounds__(256) void k_cache_append_heads(AppendArgs a, int pe
         x[0] *= rstd * g0.x; x[1] *= rstd * g0.y; x[2] *= rstd * g0.z; x[3] *= rstd * g0.w;
         x[4] *= rstd * g1.x; x[5] *= rstd * g1.y; x[6] *= rstd * g1.z; x[7] *= rstd * g1.w;
       }
+      if (a.theta > 0.f) {   // (not by an angle of zero: zero times infinity is NaN)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float p = x[e], q = x[4 + e];
-        x[e] = p * cs[e] - q * sn[e];
-        x[4 + e] = q * cs[e] + p * sn[e];
+        for (int e = 0; e < 4; ++e) {
+          const float p = x[e], q = x[4 + e];
+          x[e] = p * cs[e] - q * sn[e];
+          x[4 + e] = q * cs[e] + p * sn[e];
+        }
       }
       if (head < heads && (is_q || page >= 0)) {
         Tio* out = is_q ? (Tio*)a.Qout + (int64_t)t * a.ldqo + head * kDh

@@ -108,3 +108,21 @@ def test_fp32_attention_rows_that_begin_between_16_bytes(dh, offset, pad):
     ws = s.workspace()
     zb.zo_attention_paged(s.batch, q, ld, 4, dh ** -0.5, s.cache, o, ld, ws[0], ws[1])
     assert torch.equal(o[:, :4 * dh], plain) and (o[:, 4 * dh:] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dh", [64, 128, 256, 8])
+def test_append_without_rotation_takes_infinities_as_they_are(dtype, dh):
+    """No rotation: an infinite value turns neither itself nor its partner into NaN."""
+    s = Setup(dh, dtype, 4, 2, dh, 16, [1, 3], [20, 3])
+    for col, x in ((0, np.inf), (dh // 2 + 1, -np.inf), (4 * dh + 2, np.inf), (5 * dh + dh // 2 + 3, -np.inf)):
+        s.qkv[:, col] = x
+    s.append(None, None, 0.0)
+    assert torch.equal(s.out, s.q)
+    for i, pos, t in ((0, 19, 0), (1, 0, 1), (1, 2, 3)):
+        for pool, rows in ((s.K, s.k), (s.V, s.v)):
+            assert torch.equal(pool[int(s.table[i, pos // 16]), :, pos % 16].reshape(-1), rows[t])
+    gain = torch.ones(dh, device=DEV)
+    s.append(gain, gain, 0.0)                                  # the norm: 1 / inf of the others, NaN of the infinite one alone
+    got = _np(s.out)[:, :dh]
+    assert np.isnan(got[:, 0]).all() and (got[:, 1:dh // 2 + 1] == 0).all()
