@@ -79,6 +79,13 @@ __device__ __forceinline__ Place place_of_row(const int32_t* cu, const int32_t* 
 
 // ------------------------------------------------------------------ append
 
+// A pair turned by an angle; which product is rounded is written out, so that a pair has the same bits in every kernel.
+__device__ __forceinline__ void rotate(float& lo, float& hi, float sn, float cs) {
+  const float p = lo, q = hi;
+  lo = __builtin_fmaf(p, cs, -(q * sn));
+  hi = __builtin_fmaf(q, cs, p * sn);
+}
+
 // Any even head dimension up to 256: one wave per (row, head), lane l holds the pairs l and l + 64.  Heads 0..H-1 are
 // queries, the next Hkv keys, the last Hkv values.
 template <typename Tio>
@@ -133,10 +140,7 @@ __global__ __launch_bounds__(256) void k_cache_append(AppendArgs a) {
       if (i >= half) continue;
       double dsn, dcs;
       sincos((double)pos * exp2(-(double)(2 * i) / (double)dh * log2((double)a.theta)), &dsn, &dcs);
-      const float sn = (float)dsn, cs = (float)dcs;
-      const float p = lo[c], q = hi[c];
-      lo[c] = p * cs - q * sn;
-      hi[c] = q * cs + p * sn;
+      rotate(lo[c], hi[c], (float)dsn, (float)dcs);
     }
   }
 #pragma unroll
@@ -176,10 +180,17 @@ __global__ __launch_bounds__(256) void k_cache_append_heads(AppendArgs a, int pe
   const int j = lane % kLanes, hh = lane / kLanes;
   const int nkv = a.c.n_kv_heads, heads = a.n_heads + 2 * nkv;
   const int g_first = blockIdx.y * per_wave, g_last = min(g_first + per_wave, (heads + kHeads - 1) / kHeads);
-  double freq[4];   // revolutions per position
+  // bf16: the lane's four pairs, revolutions per position.  fp32: radians per position, formed as in the other kernels of this
+  // rotation, a row's angles spread over the wave's lanes (a sine in double precision is dear): lane l has l kOwn .. l kOwn + kOwn - 1.
+  constexpr bool kExact = sizeof(Tio) == 4;
+  constexpr int kOwn = kDh > 128 ? kDh / 128 : 1, kFreqs = kExact ? kOwn : 4;
+  double freq[kFreqs];
   if (a.theta > 0.f) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) freq[e] = exp2(-(double)(2 * (4 * j + e)) / kDh * log2_theta) * 0.15915494309189533577;
+    for (int e = 0; e < kFreqs; ++e) {
+      if constexpr (kExact) freq[e] = exp2(-(double)(2 * ((lane * kOwn + e) % (kDh / 2))) / (double)kDh * log2((double)a.theta));
+      else freq[e] = exp2(-(double)(2 * (4 * j + e)) / kDh * log2_theta) * 0.15915494309189533577;
+    }
   }
   float4 gq0 = make_float4(1.f, 1.f, 1.f, 1.f), gq1 = gq0, gk0 = gq0, gk1 = gq0;
   if (a.gamma_q) {
@@ -204,12 +215,28 @@ __global__ __launch_bounds__(256) void k_cache_append_heads(AppendArgs a, int pe
     const int page = page_of(a.c, pl.seq, pl.pos);
     float cs[4], sn[4];
     if (a.theta > 0.f) {
+      if constexpr (kExact) {
+        float own_sn[kOwn], own_cs[kOwn];   // rounded once: 6e-8
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const double turns = (double)pl.pos * freq[e];
-        const float part = (float)(turns - floor(turns));   // (the hardware's sine and cosine take revolutions)
-        cs[e] = __builtin_amdgcn_cosf(part);
-        sn[e] = __builtin_amdgcn_sinf(part);
+        for (int e = 0; e < kOwn; ++e) {
+          double dsn, dcs;
+          sincos((double)pl.pos * freq[e], &dsn, &dcs);
+          own_sn[e] = (float)dsn;
+          own_cs[e] = (float)dcs;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          sn[e] = __shfl(own_sn[e % kOwn], (4 * j + e) / kOwn);
+          cs[e] = __shfl(own_cs[e % kOwn], (4 * j + e) / kOwn);
+        }
+      } else {   // the hardware's sine and cosine, which take revolutions: 3e-7, under bf16's 4e-3
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const double turns = (double)pl.pos * freq[e];
+          const float part = (float)(turns - floor(turns));
+          cs[e] = __builtin_amdgcn_cosf(part);
+          sn[e] = __builtin_amdgcn_sinf(part);
+        }
       }
     }
     for (int grp = g_first; grp < g_last; ++grp) {
@@ -233,11 +260,7 @@ __global__ __launch_bounds__(256) void k_cache_append_heads(AppendArgs a, int pe
       }
       if (a.theta > 0.f) {   // (not by an angle of zero: zero times infinity is NaN)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float p = x[e], q = x[4 + e];
-          x[e] = p * cs[e] - q * sn[e];
-          x[4 + e] = q * cs[e] + p * sn[e];
-        }
+        for (int e = 0; e < 4; ++e) rotate(x[e], x[4 + e], sn[e], cs[e]);
       }
       if (head < heads && (is_q || page >= 0)) {
         Tio* out = is_q ? (Tio*)a.Qout + (int64_t)t * a.ldqo + head * kDh

@@ -126,3 +126,33 @@ def test_append_without_rotation_takes_infinities_as_they_are(dtype, dh):
     s.append(gain, gain, 0.0)                                  # the norm: 1 / inf of the others, NaN of the infinite one alone
     got = _np(s.out)[:, :dh]
     assert np.isnan(got[:, 0]).all() and (got[:, 1:dh // 2 + 1] == 0).all()
+
+
+@pytest.mark.parametrize("dh", [64, 128, 256])
+def test_fp32_rotation_does_not_depend_on_the_path(dh):
+    """Without a norm a rotated pair is two products of the row and the rounded sine and cosine: aligned rows, rows that begin
+    between 16 bytes and the packed prompt's rotation give the same bits."""
+    H, g, n, far = 4, 2, 300, 131072 - 40
+    for past in (0, far):
+        kv = [n + past]
+        s = Setup(dh, "f32", H, g, dh, 1024, [n], kv)
+        s.append(None, None, 1e4)
+        a, ka = s.out.clone(), s.K.clone()
+        odd = torch.empty(n, s.ld + 1, device=DEV)[:, 1:]
+        odd.copy_(s.qkv)
+        out = torch.empty(n, H * dh, device=DEV)
+        ld = odd.stride(0)
+        s.K.zero_()
+        zb.zo_cache_append(s.batch, odd, ld, odd[:, H * dh:], ld, odd[:, (H + g) * dh:], ld, H, None, None, 0.0, 1e4, s.cache, out, H * dh)
+        page = [int(s.table[0, p // 1024]) for p in range(past, past + n)]
+        at = (torch.tensor(page, device=DEV), slice(None), torch.arange(past, past + n, device=DEV) % 1024)
+        assert torch.equal(a[:, :H * dh], out) and torch.equal(ka[at], s.K[at])
+        if past == 0:
+            qkv = s.qkv.clone()
+            zb.zo_qk_norm_rope(s.batch, qkv, s.ld, qkv[:, H * dh:], s.ld, H, g, dh, None, None, 0.0, 1e4, zb.ZO_F32)
+            assert torch.equal(qkv[:, :H * dh], out)
+        # a rounded sine and cosine (u of 1 each), two products and a sum: 3 u of the pair's length
+        q, _, _ = od.cache_append(_np(s.q), _np(s.k), _np(s.v), s.cu, H, None, None, 0.0, 1e4, _np(s.K), _np(s.V), s.table, kv)
+        w = q.reshape(n, H, 2, dh // 2)
+        tol = 3.01 * U * np.hypot(w[:, :, 0], w[:, :, 1])[:, :, None]
+        assert (np.abs(_np(out).reshape(w.shape) - w) <= tol).all()
