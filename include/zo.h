@@ -535,6 +535,7 @@ int32_t zo_sample(const void* logits, int64_t ld, int32_t n_rows, int32_t vocab,
  *   tokens int32 [n_rows];  pos int32 [n_rows] (may be NULL when neither E_pos nor pos_next is given)
  *   E [vocab x d] ld lde, E_pos [n_pos x d] ld ldp (NULL: none), X [n_rows x d] ld ldx, of type dtype
  *   pos_next int32 [n_rows] (may be NULL; may be pos itself, e.g. the kv_len of a decode loop)
+ *   d = 0: no rows, the positions alone are advanced (E and X may be NULL)
  * No workspace.
  */
 int32_t zo_embed_rows(const int32_t* tokens, const int32_t* pos, int32_t n_rows, const void* E, int64_t lde,

@@ -345,7 +345,7 @@ class DecodeDriver:
         b0 = model.blocks[0].blk
         self.cache = DeviceCache(len(model.blocks), S, int(lens.max()) + int(max_new), b0.n_kv_heads, b0.head_dim, d.dtype, dev,
                                  page_size)
-        self.lens = torch.from_numpy(lens.astype(np.int32)).to(dev)
+        self.before = torch.from_numpy((lens - 1).astype(np.int32)).to(dev)
         self.last = torch.from_numpy((d.batch.host["cu"][1:] - 1).astype(np.int32)).to(dev)
         # the same layers, weights and candidates on one row per sequence
         self.rows = copy.copy(d)
@@ -391,7 +391,9 @@ class DecodeDriver:
 
     def prefill(self, stream=None):
         """Runs the prompts (the workload's input rows) into the caches and draws every sequence's first token."""
-        self.cache.kv_len.copy_(self.lens)
+        # the caches' lengths, on the stream that the appends run on (no rows: the positions alone are advanced)
+        zb.zo_embed_rows(self.last, self.before, self.S, None, 0, 0, None, 0, 0, 0, _dt(self.d.dtype), None, 0,
+                         self.cache.kv_len, stream)
         self._blocks(self.prompt_blocks, self.d.X, self.prompt_final, stream)
         f = self.prompt_final
         zb.zo_embed_rows(self.last, None, self.S, f, f.stride(0), f.shape[0], None, 0, 0, self.hidden, _dt(self.d.dtype),

@@ -1,0 +1,60 @@
+"""The decode driver's bookkeeping without a GPU: tensors on the host, and a library that notes the calls and does nothing."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2605_28760_amd import binding as zb
+from paper_2605_28760_amd import workloads as wl
+from paper_2605_28760_amd.runner import DecodeDriver, DeviceModel, DeviceWorkload
+
+
+class Recorder:
+    """Workspace queries are the library's own; every other call is noted and succeeds."""
+
+    def __init__(self, real):
+        self.real, self.calls = real, []
+
+    def __getattr__(self, name):
+        fn = getattr(self.real, name)
+        if name.endswith("_bytes"):
+            return fn
+
+        def call(*args):
+            self.calls.append((name, args))
+            return zb.ZO_OK
+        return call
+
+
+@pytest.fixture
+def recorder(monkeypatch):
+    r = Recorder(zb.lib())
+    monkeypatch.setattr(zb, "_lib", r)
+    return r
+
+
+def _workload(cfg=40, R_used=None):
+    w = wl.decoder_model("dec-host", cfg, "bf16", 2, 256, 2, 1, 128, 384, 777, 1, False, 8, 1e-2, 32,
+                         wl._pair_batch([33, 5, 64], [0, 1, 0], 2, [20, 1]), qwen=True)
+    for l in w.layers:
+        l.R_used = l.P.shape[1] if R_used is None else R_used
+    return w
+
+
+def test_prefill_leaves_everything_to_its_stream(recorder):
+    """The lengths of the caches are set by a call on the stream that the appends run on, not by an operation of torch's."""
+    dec = DecodeDriver(DeviceModel(DeviceWorkload(_workload(), "cpu")), 4, page_size=16)
+    kv = dec.cache.kv_len
+    kv.fill_(99)
+    dec.prefill(0x1230)
+    dec.step(0x1230)
+    assert (kv == 99).all()
+    assert all(args[-1] == 0x1230 for _, args in recorder.calls)
+    names = [n for n, _ in recorder.calls]
+    setting = [i for i, (n, args) in enumerate(recorder.calls) if n == "zo_embed_rows" and args[13] == kv.data_ptr()]
+    assert len(setting) == 2 and setting[0] < names.index("zo_cache_append")
+    pos = recorder.calls[setting[0]][1][1]
+    at = (C.c_int32 * dec.S).from_address(pos)
+    assert list(at) == [n - 1 for n in np.diff(dec.d.batch.host["cu"])]

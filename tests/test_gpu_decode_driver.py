@@ -1,0 +1,61 @@
+"""The decode driver on streams given as arguments, under candidates that change after it was built, and with banks that grow."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from paper_2605_28760_amd import workloads as wl
+from paper_2605_28760_amd.runner import DecodeDriver, DeviceModel, DeviceWorkload
+from test_gpu_decode_loop import DEV, _model
+
+
+def _answer(dec, steps=4, stream=None):
+    """Logits and tokens of prompts and steps, and the caches, with fixed uniforms."""
+    out = []
+    for n in range(steps):
+        torch.cuda.synchronize()
+        dec.u.fill_(0.15 + 0.2 * n)
+        torch.cuda.synchronize()
+        dec.prefill(stream) if n == 0 else dec.step(stream)
+        torch.cuda.synchronize()
+        out += [dec.logits.clone(), dec.tokens.clone()]
+    return out + [dec.cache.kv_len.clone()]
+
+
+def _same(a, b):
+    return all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_prefill_on_a_stream_of_its_own():
+    """Only the stream that is passed orders the call: work that is waiting on the current one does not come into it."""
+    w = _model("bf16", True, 70)
+    new = lambda: DecodeDriver(DeviceModel(DeviceWorkload(w, DEV)), 12, temperature=0.8, top_k=40, page_size=16)
+    want = _answer(new())
+    dec, side = new(), torch.cuda.Stream(device=DEV)
+    x = torch.randn(8192, 8192, device=DEV)
+    dec.u.fill_(0.15)
+    torch.cuda.synchronize()
+    for _ in range(8):
+        y = x @ x                                # the current stream is busy for tens of milliseconds
+    dec.prefill(side)
+    got = []
+    for n in range(4):
+        if n:
+            dec.step(side)
+        side.synchronize()
+        with torch.cuda.stream(side):
+            got += [dec.logits.clone(), dec.tokens.clone()]
+            dec.u.fill_(0.15 + 0.2 * (n + 1))
+    side.synchronize()
+    assert _same(got, want[:-1])
+    with torch.cuda.stream(side):                # and a second answer after the first, inside the stream's context
+        dec.u.fill_(0.15)
+        dec.prefill(side)
+        first = dec.logits.clone()
+        dec.step(side)
+        kv = dec.cache.kv_len.clone()
+    side.synchronize()
+    assert torch.equal(first, want[0]) and torch.equal(kv, want[-1] - 2)
+    torch.cuda.synchronize()
+    del y
