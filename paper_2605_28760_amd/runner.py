@@ -46,6 +46,17 @@ class DeviceBatch:
                                     mir["cu"], mir["seq_cand"], mir["cand_dir"],
                                     n_seqs=self.S, n_cands=self.C, n_dirs=self.K, dir_seed_v=self.dir_seed_v)
 
+    def one_row_each(self):
+        """The same sequences under the same candidates, one row per sequence: the candidate table and the seeds are this
+        batch's own tensors, so what is written to them later holds for both."""
+        b = copy.copy(self)
+        b.host = dict(self.host, cu=np.arange(self.S + 1, dtype=np.int32))
+        b.cu, b.T = torch.from_numpy(b.host["cu"]).to(self.cu.device), self.S
+        mir = b.host if self.struct.host_seq_cand else dict(seq_cand=None, cand_dir=None)
+        b.struct = zb.make_batch(b.T, b.cu, b.seq_cand, b.cand_dir, b.cand_sign, b.dir_seed, b.host["cu"], mir["seq_cand"],
+                                 mir["cand_dir"], n_seqs=b.S, n_cands=b.C, n_dirs=b.K, dir_seed_v=b.dir_seed_v)
+        return b
+
 
 class DeviceLayer:
     def __init__(self, layer, dtype, device):
@@ -349,7 +360,7 @@ class DecodeDriver:
         self.last = torch.from_numpy((d.batch.host["cu"][1:] - 1).astype(np.int32)).to(dev)
         # the same layers, weights and candidates on one row per sequence
         self.rows = copy.copy(d)
-        self.rows.batch = DeviceBatch(np.arange(S + 1), w.seq_cand, w.cand_dir, w.cand_sign, w.dir_seed, dev)
+        self.rows.batch = d.batch.one_row_each()
         self.rows.Y = [torch.empty((S, y.shape[1]), device=dev, dtype=y.dtype) for y in d.Y]
         self.plain = DeviceBatch(np.arange(S + 1), np.full(S, -1), np.zeros(0), np.zeros(0), np.zeros(0, np.uint64), dev)
         ws = zb.zo_probe_linear_workspace_bytes(S, S, 0, d.head.shape[0], self.hidden, 1, 0, _dt(d.dtype))

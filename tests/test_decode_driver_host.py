@@ -58,3 +58,18 @@ def test_prefill_leaves_everything_to_its_stream(recorder):
     pos = recorder.calls[setting[0]][1][1]
     at = (C.c_int32 * dec.S).from_address(pos)
     assert list(at) == [n - 1 for n in np.diff(dec.d.batch.host["cu"])]
+
+
+@pytest.mark.parametrize("mirrors", [True, False])
+def test_decode_rows_are_under_the_tensors_of_the_models_batch(recorder, mirrors):
+    d = DeviceWorkload(_workload(), "cpu", host_mirrors=mirrors)
+    d.batch.dir_seed_v = d.batch.dir_seed.clone()
+    d.batch.struct.dir_seed_v = d.batch.dir_seed_v.data_ptr()
+    dec = DecodeDriver(DeviceModel(d), 4, page_size=16)
+    a, b = d.batch.struct, dec.rows.batch.struct
+    for field in ("seq_cand", "cand_dir", "cand_sign", "dir_seed", "dir_seed_v", "n_seqs", "n_cands", "n_dirs", "host_seq_cand",
+                  "host_cand_dir"):
+        assert getattr(a, field) == getattr(b, field), field
+    assert b.n_tokens == b.n_seqs == d.batch.S and list(dec.rows.batch.cu) == list(range(d.batch.S + 1))
+    assert list((C.c_int32 * (d.batch.S + 1)).from_address(b.host_cu_seqlens)) == list(range(d.batch.S + 1))
+    assert a.n_tokens == d.batch.T and d.batch.host["cu"][-1] == d.batch.T      # the model's batch is as it was

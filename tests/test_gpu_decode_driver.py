@@ -59,3 +59,19 @@ def test_prefill_on_a_stream_of_its_own():
     assert torch.equal(first, want[0]) and torch.equal(kv, want[-1] - 2)
     torch.cuda.synchronize()
     del y
+
+
+def test_steps_follow_the_candidates_that_the_batch_holds():
+    """Seeds and signs written to the model's batch after the driver was built reach prompts and steps alike."""
+    w = _model("bf16", True, 71)
+    d = DeviceWorkload(w, DEV)
+    dec = DecodeDriver(DeviceModel(d), 6, temperature=0.0, page_size=16)
+    before = _answer(dec)
+    w2 = _model("bf16", True, 71)
+    w2.dir_seed = w.dir_seed + np.uint64(1000)
+    w2.cand_sign = -w.cand_sign
+    d.batch.dir_seed.copy_(torch.from_numpy(w2.dir_seed.view(np.int64)))
+    d.batch.cand_sign.copy_(torch.from_numpy(w2.cand_sign))
+    got = _answer(dec)
+    assert _same(got, _answer(DecodeDriver(DeviceModel(DeviceWorkload(w2, DEV)), 6, temperature=0.0, page_size=16)))
+    assert not torch.equal(got[0], before[0]) and not torch.equal(got[2], before[2])
