@@ -363,12 +363,17 @@ class DecodeDriver:
         self.rows.batch = d.batch.one_row_each()
         self.rows.Y = [torch.empty((S, y.shape[1]), device=dev, dtype=y.dtype) for y in d.Y]
         self.plain = DeviceBatch(np.arange(S + 1), np.full(S, -1), np.zeros(0), np.zeros(0), np.zeros(0, np.uint64), dev)
-        ws = zb.zo_probe_linear_workspace_bytes(S, S, 0, d.head.shape[0], self.hidden, 1, 0, _dt(d.dtype))
-        for l in d.layers:
-            R = l.bank.R_used if l.bank is not None else 0
-            ws = max(ws, zb.zo_probe_linear_workspace_bytes(S, S, self.rows.batch.K, l.m, l.n, w.r, R, _dt(d.dtype)))
+        # workspaces for the banks at their full width: updates may widen them later
+        def linears(batch):
+            return max(zb.zo_probe_linear_workspace_bytes(batch.T, S, batch.K, l.m, l.n, w.r,
+                                                          l.bank.R_cap if l.bank is not None else 0, _dt(d.dtype)) for l in d.layers)
+        ws = max(linears(self.rows.batch),
+                 zb.zo_probe_linear_workspace_bytes(S, S, 0, d.head.shape[0], self.hidden, 1, 0, _dt(d.dtype)))
         self.rows.ws_bytes, self.rows.ws = ws, torch.empty(max(ws, 256), device=dev, dtype=torch.uint8)
-        self.prompt_blocks = [CachedBlock(d, blk.blk, blk.base, c, True) for blk, c in zip(model.blocks, self.cache.structs)]
+        self.prompts, ws = copy.copy(d), linears(d.batch)
+        if ws > d.ws_bytes:
+            self.prompts.ws_bytes, self.prompts.ws = ws, torch.empty(ws, device=dev, dtype=torch.uint8)
+        self.prompt_blocks = [CachedBlock(self.prompts, blk.blk, blk.base, c, True) for blk, c in zip(model.blocks, self.cache.structs)]
         self.blocks = [CachedBlock(self.rows, blk.blk, blk.base, c, False) for blk, c in zip(model.blocks, self.cache.structs)]
         self.gf, self.bf = model.gf, model.bf
         new = lambda shape, dt: torch.empty(shape, device=dev, dtype=dt)

@@ -73,3 +73,20 @@ def test_decode_rows_are_under_the_tensors_of_the_models_batch(recorder, mirrors
     assert b.n_tokens == b.n_seqs == d.batch.S and list(dec.rows.batch.cu) == list(range(d.batch.S + 1))
     assert list((C.c_int32 * (d.batch.S + 1)).from_address(b.host_cu_seqlens)) == list(range(d.batch.S + 1))
     assert a.n_tokens == d.batch.T and d.batch.host["cu"][-1] == d.batch.T      # the model's batch is as it was
+
+
+def test_workspaces_have_room_for_the_whole_banks(recorder):
+    """A bank that is widened after the driver was built (up to its capacity) fits into what the driver passes."""
+    d = DeviceWorkload(_workload(R_used=8), "cpu")
+    dec = DecodeDriver(DeviceModel(d), 4, page_size=16)
+    for l in d.layers:
+        l.bank.R_used = l.bank.R_cap
+    dec.prefill()
+    dec.step()
+    linears = [args for n, args in recorder.calls if n == "zo_probe_linear"]
+    assert len(linears) == 2 * (len(d.layers) + 1)
+    for args in linears:
+        batch, bank = args[0]._obj, args[12]._obj if args[12] is not None else None
+        need = zb.zo_probe_linear_workspace_bytes(batch.n_tokens, batch.n_seqs, batch.n_dirs, args[6], args[7], args[9],
+                                                  bank.R_used if bank else 0, args[8])
+        assert args[18] >= need, (batch.n_tokens, args[6], args[7], args[18], need)

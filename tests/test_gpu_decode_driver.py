@@ -75,3 +75,18 @@ def test_steps_follow_the_candidates_that_the_batch_holds():
     got = _answer(dec)
     assert _same(got, _answer(DecodeDriver(DeviceModel(DeviceWorkload(w2, DEV)), 6, temperature=0.0, page_size=16)))
     assert not torch.equal(got[0], before[0]) and not torch.equal(got[2], before[2])
+
+
+def test_a_bank_that_grows_after_the_driver_was_built():
+    w = _model("bf16", True, 72)
+    for l in w.layers:
+        l.R_used = 16
+    d = DeviceWorkload(w, DEV)
+    dec = DecodeDriver(DeviceModel(d), 6, temperature=0.0, page_size=16)
+    for l in d.layers:
+        l.bank.R_used = l.bank.R_cap
+    got = _answer(dec)
+    w2 = _model("bf16", True, 72)
+    for l in w2.layers:
+        l.R_used = l.P.shape[1]
+    assert _same(got, _answer(DecodeDriver(DeviceModel(DeviceWorkload(w2, DEV)), 6, temperature=0.0, page_size=16)))
