@@ -333,16 +333,22 @@ class DecodeDriver:
 
     embed  [vocab, hidden] token embeddings (default: the head's rows), positions [n, hidden] learned positions or None.
     temperature, top_k, top_p, min_p: a number for all sequences or one per sequence; None: no limit.
+    batch  the candidates that the sequences answer under: a DeviceBatch of the model's sequences (default: the model's own; a
+           LoopDriver's, for the directions of its present step).  Prompts and steps read its candidate table and seeds as
+           they are when they run.
     Everything a step reads lies on the device, so one captured graph replays every step; the caller fills `u` before each
     draw and reads `tokens` after it.  The caches have room for max_new tokens behind the longest prompt: what follows them is
     not stored."""
 
     def __init__(self, model, max_new, embed=None, positions=None, temperature=1.0, top_k=None, top_p=None, min_p=None,
-                 page_size=64):
+                 page_size=64, batch=None):
         d = self.d = model.d
         w, dev = d.w, d.device
-        S = self.S = d.batch.S
-        lens = np.diff(d.batch.host["cu"])
+        batch = self.batch = d.batch if batch is None else batch
+        if not np.array_equal(batch.host["cu"], d.batch.host["cu"]):
+            raise ValueError("batch: other sequences than the model's")
+        S = self.S = batch.S
+        lens = np.diff(batch.host["cu"])
         if (lens < 1).any():
             raise ValueError("every sequence needs a prompt of at least one token")
         if len({(blk.blk.n_kv_heads, blk.blk.head_dim) for blk in model.blocks}) != 1:
@@ -357,10 +363,10 @@ class DecodeDriver:
         self.cache = DeviceCache(len(model.blocks), S, int(lens.max()) + int(max_new), b0.n_kv_heads, b0.head_dim, d.dtype, dev,
                                  page_size)
         self.before = torch.from_numpy((lens - 1).astype(np.int32)).to(dev)
-        self.last = torch.from_numpy((d.batch.host["cu"][1:] - 1).astype(np.int32)).to(dev)
+        self.last = torch.from_numpy((batch.host["cu"][1:] - 1).astype(np.int32)).to(dev)
         # the same layers, weights and candidates on one row per sequence
         self.rows = copy.copy(d)
-        self.rows.batch = d.batch.one_row_each()
+        self.rows.batch = batch.one_row_each()
         self.rows.Y = [torch.empty((S, y.shape[1]), device=dev, dtype=y.dtype) for y in d.Y]
         self.plain = DeviceBatch(np.arange(S + 1), np.full(S, -1), np.zeros(0), np.zeros(0), np.zeros(0, np.uint64), dev)
         # workspaces for the banks at their full width: updates may widen them later
@@ -370,14 +376,15 @@ class DecodeDriver:
         ws = max(linears(self.rows.batch),
                  zb.zo_probe_linear_workspace_bytes(S, S, 0, d.head.shape[0], self.hidden, 1, 0, _dt(d.dtype)))
         self.rows.ws_bytes, self.rows.ws = ws, torch.empty(max(ws, 256), device=dev, dtype=torch.uint8)
-        self.prompts, ws = copy.copy(d), linears(d.batch)
+        self.prompts, ws = copy.copy(d), linears(batch)
+        self.prompts.batch = batch
         if ws > d.ws_bytes:
             self.prompts.ws_bytes, self.prompts.ws = ws, torch.empty(ws, device=dev, dtype=torch.uint8)
         self.prompt_blocks = [CachedBlock(self.prompts, blk.blk, blk.base, c, True) for blk, c in zip(model.blocks, self.cache.structs)]
         self.blocks = [CachedBlock(self.rows, blk.blk, blk.base, c, False) for blk, c in zip(model.blocks, self.cache.structs)]
         self.gf, self.bf = model.gf, model.bf
         new = lambda shape, dt: torch.empty(shape, device=dev, dtype=dt)
-        self.prompt_final, self.prompt_last = new((d.batch.T, self.hidden), _tt(d.dtype)), new((S, self.hidden), _tt(d.dtype))
+        self.prompt_final, self.prompt_last = new((batch.T, self.hidden), _tt(d.dtype)), new((S, self.hidden), _tt(d.dtype))
         self.x, self.final = (new((S, self.hidden), _tt(d.dtype)) for _ in range(2))
         self.logits = new((S, d.head.shape[0]), torch.float32)
         self.tokens, self.n_kept = new(S, torch.int32), new(S, torch.int32)

@@ -8,7 +8,7 @@ torch = pytest.importorskip("torch")
 
 from paper_2605_28760_amd import binding as zb
 from paper_2605_28760_amd import workloads as wl
-from paper_2605_28760_amd.runner import DecodeDriver, DeviceModel, DeviceWorkload
+from paper_2605_28760_amd.runner import DecodeDriver, DeviceBatch, DeviceModel, DeviceWorkload
 
 
 class Recorder:
@@ -90,3 +90,19 @@ def test_workspaces_have_room_for_the_whole_banks(recorder):
         need = zb.zo_probe_linear_workspace_bytes(batch.n_tokens, batch.n_seqs, batch.n_dirs, args[6], args[7], args[9],
                                                   bank.R_used if bank else 0, args[8])
         assert args[18] >= need, (batch.n_tokens, args[6], args[7], args[18], need)
+
+
+def test_another_batch_has_the_models_sequences(recorder):
+    w = _workload()
+    model = DeviceModel(DeviceWorkload(w, "cpu"))
+    b = model.d.batch
+    make = lambda cu, seq_cand: DeviceBatch(cu, seq_cand, b.host["cand_dir"], w.cand_sign, w.dir_seed, "cpu")
+    for cu, sc in ((b.host["cu"] + (np.arange(b.S + 1) == 1), b.host["seq_cand"]), (b.host["cu"][:-1], b.host["seq_cand"][:-1])):
+        with pytest.raises(ValueError, match="sequences"):
+            DecodeDriver(model, 4, page_size=16, batch=make(cu, sc))
+    other = make(b.host["cu"], b.host["seq_cand"])
+    dec = DecodeDriver(model, 4, page_size=16, batch=other)
+    dec.prefill()
+    dec.step()
+    seeds = {args[0]._obj.dir_seed for n, args in recorder.calls if n == "zo_probe_linear" and args[0]._obj.n_dirs}
+    assert seeds == {other.dir_seed.data_ptr()} and model.d.batch is b

@@ -6,7 +6,7 @@ torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
 from paper_2605_28760_amd import workloads as wl
-from paper_2605_28760_amd.runner import DecodeDriver, DeviceModel, DeviceWorkload
+from paper_2605_28760_amd.runner import DecodeDriver, DeviceBatch, DeviceModel, DeviceWorkload
 from test_gpu_decode_loop import DEV, _model
 
 
@@ -90,3 +90,19 @@ def test_a_bank_that_grows_after_the_driver_was_built():
     for l in w2.layers:
         l.R_used = l.P.shape[1]
     assert _same(got, _answer(DecodeDriver(DeviceModel(DeviceWorkload(w2, DEV)), 6, temperature=0.0, page_size=16)))
+
+
+def test_answers_under_another_batch_of_candidates():
+    """A batch of the same sequences with candidates of its own (two seeds per direction): prompts and steps run under it."""
+    w = _model("bf16", True, 73)
+    d = DeviceWorkload(w, DEV)
+    b = d.batch
+    seeds = w.dir_seed + np.uint64(5)
+    other = DeviceBatch(b.host["cu"], b.host["seq_cand"], b.host["cand_dir"], w.cand_sign, w.dir_seed, DEV, dir_seed_v=seeds)
+    got = _answer(DecodeDriver(DeviceModel(d), 6, temperature=0.0, page_size=16, batch=other))
+    d2 = DeviceWorkload(w, DEV)
+    d2.batch = other
+    want = _answer(DecodeDriver(DeviceModel(d2), 6, temperature=0.0, page_size=16))
+    assert _same(got, want)
+    own = _answer(DecodeDriver(DeviceModel(d), 6, temperature=0.0, page_size=16))
+    assert not torch.equal(got[0], own[0]) and not torch.equal(got[2], own[2])
