@@ -469,8 +469,8 @@ typedef struct zo_cache {
  *   Qout[t] = q;  K[page][g][slot] = k, V[page][g][slot] = v of kv head g
  * Of `batch` only n_tokens, n_seqs and cu_seqlens are read.  Q, Qout: [n_tokens x n_heads*head_dim];
  * K, V: [n_tokens x n_kv_heads*head_dim], of the cache's dtype; the three may be column ranges of one
- * fused projection output.  Qout may be Q itself (same pointer and leading dimension); otherwise it
- * overlaps none of the inputs.  head_dim even, <= 256; one rounding to dtype.  Angles are formed in
+ * fused projection output.  Qout may be Q itself (same pointer and leading dimension; with neither norm nor
+ * rotation the queries are then not touched); otherwise it overlaps none of the inputs.  head_dim even, <= 256; one rounding to dtype.  Angles are formed in
  * double precision, so that far positions keep theirs.  No workspace.
  * Refused with ZO_ERR_INDEX where the host copies show it: a kv_len smaller than the sequence's rows
  * or beyond its pages, a page of a position in use outside the pool.

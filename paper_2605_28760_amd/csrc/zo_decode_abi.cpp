@@ -143,6 +143,7 @@ int32_t zo_cache_append(const zo_batch* batch, const void* Q, int64_t ldq, const
   a.cu = batch->cu_seqlens; a.S = batch->n_seqs; a.T = batch->n_tokens; a.n_heads = n_heads;
   a.gamma_q = gamma_q; a.gamma_k = gamma_k; a.eps = norm_eps; a.theta = rope_theta > 0.0f ? rope_theta : 0.0f;
   a.c = to_dev(cache);
+  if (Qout == Q && !gamma_q && a.theta == 0.0f) a.n_heads = 0;   // (queries that stay as and where they are)
   ZO_HIP(zo::launch_cache_append(a, (hipStream_t)stream), "zo_cache_append");
   return ZO_OK;
 }

@@ -313,7 +313,7 @@ struct AppendArgs {
   const void* V; int64_t ldv;
   void* Qout; int64_t ldqo;         // may be Q
   const int32_t* cu; int S, T;
-  int n_heads;
+  int n_heads;                      // 0: keys and values alone
   const float* gamma_q; const float* gamma_k;   // both null: no norm
   float eps;
   float theta;                      // <= 0: no rotation

@@ -303,7 +303,7 @@ class CachedBlock(DeviceBlock):
         super().__init__(d, blk, base)
         self.cache, self.prompt = cache, prompt
         b = self.blk
-        self.q = torch.empty_like(self.att)
+        self.q = None if prompt else torch.empty_like(self.att)
         self.ws_bytes = 0 if prompt else zb.zo_attention_paged_workspace_bytes(
             d.batch.T, b.n_heads, b.head_dim, cache.max_pages * cache.page_size, _dt(d.dtype))
         self.ws = torch.empty(max(self.ws_bytes, 256), device=d.device, dtype=torch.uint8)
@@ -316,9 +316,11 @@ class CachedBlock(DeviceBlock):
         b, d = self.blk, self.d
         batch = batch or d.batch
         nq, nkv, ld = b.n_heads * b.head_dim, b.n_kv_heads * b.head_dim, qkv.stride(0)
+        # (a prompt's rows come normed and rotated: in place, so that only keys and values move)
         gq, gk, theta = (None, None, 0.0) if self.prompt else (self.gq, self.gk, float(self.rope_theta or 0.0))
+        q, ldq = (qkv, ld) if self.prompt else (self.q, nq)
         zb.zo_cache_append(batch.struct, qkv, ld, qkv[:, nq:], ld, qkv[:, nq + nkv:], ld, b.n_heads, gq, gk,
-                           float(b.norm_eps), theta, self.cache, self.q, nq, stream)
+                           float(b.norm_eps), theta, self.cache, q, ldq, stream)
         if self.prompt:
             super().attention(qkv, out, stream, batch)
         else:

@@ -156,3 +156,15 @@ def test_fp32_rotation_does_not_depend_on_the_path(dh):
         w = q.reshape(n, H, 2, dh // 2)
         tol = 3.01 * U * np.hypot(w[:, :, 0], w[:, :, 1])[:, :, None]
         assert (np.abs(_np(out).reshape(w.shape) - w) <= tol).all()
+
+
+@pytest.mark.parametrize("dh", [128, 8])
+def test_append_in_place_without_norm_and_rotation_leaves_the_queries(dh):
+    """Not even a signalling NaN is made quiet; keys and values go to their slots, the rest of the pools stays."""
+    s = Setup(dh + 1, "bf16", 4, 2, dh, 16, [1, 0, 40], [20, 0, 40], extra_rows=1)
+    s.qkv[:, :4 * dh] = torch.tensor([0x7F81], dtype=torch.int16, device=DEV).view(torch.bfloat16)
+    bits, K0, V0 = s.qkv.view(torch.int16).clone(), _np(s.K), _np(s.V)
+    s.append(None, None, 0.0, out=s.qkv)
+    assert torch.equal(s.qkv.view(torch.int16), bits)
+    _, K, V = od.cache_append(np.zeros((41, 4 * dh)), _np(s.k)[:41], _np(s.v)[:41], s.cu, 4, None, None, 0.0, 0.0, K0, V0, s.table, s.kv)
+    assert (_np(s.K) == K).all() and (_np(s.V) == V).all()
