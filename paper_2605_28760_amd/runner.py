@@ -296,17 +296,19 @@ class DeviceCache:
 
 
 class CachedBlock(DeviceBlock):
-    """A DeviceBlock whose keys and values live in a cache: its rows continue their sequences there.  With `prompt` the rows
-    are whole prompts that enter an empty cache, and attention runs on the packed rows themselves."""
+    """A block of a model whose keys and values live in a cache.  With `prompt` the rows are whole prompts that enter an empty
+    cache: attention runs on the packed rows themselves, in the model block's own activations.  Otherwise they continue
+    their sequences in the cache; `scratch` is (queries, attention workspace), which the blocks of a model share, since one
+    runs after the other."""
 
-    def __init__(self, d, blk, base, cache, prompt):
-        super().__init__(d, blk, base)
+    def __init__(self, d, block, cache, prompt, scratch=None):
+        if prompt:
+            self.__dict__.update(block.__dict__)
+            self.d = d
+        else:
+            super().__init__(d, block.blk, block.base)
+            self.q, self.ws = scratch
         self.cache, self.prompt = cache, prompt
-        b = self.blk
-        self.q = None if prompt else torch.empty_like(self.att)
-        self.ws_bytes = 0 if prompt else zb.zo_attention_paged_workspace_bytes(
-            d.batch.T, b.n_heads, b.head_dim, cache.max_pages * cache.page_size, _dt(d.dtype))
-        self.ws = torch.empty(max(self.ws_bytes, 256), device=d.device, dtype=torch.uint8)
 
     def qk_norm_rope(self, qkv, stream=None, batch=None):
         if self.prompt:   # (a prompt's positions are its rows' offsets)
@@ -318,14 +320,14 @@ class CachedBlock(DeviceBlock):
         nq, nkv, ld = b.n_heads * b.head_dim, b.n_kv_heads * b.head_dim, qkv.stride(0)
         # (a prompt's rows come normed and rotated: in place, so that only keys and values move)
         gq, gk, theta = (None, None, 0.0) if self.prompt else (self.gq, self.gk, float(self.rope_theta or 0.0))
-        q, ldq = (qkv, ld) if self.prompt else (self.q, nq)
+        q, ldq = (qkv, ld) if self.prompt else (self.q, self.q.stride(0))
         zb.zo_cache_append(batch.struct, qkv, ld, qkv[:, nq:], ld, qkv[:, nq + nkv:], ld, b.n_heads, gq, gk,
                            float(b.norm_eps), theta, self.cache, q, ldq, stream)
         if self.prompt:
             super().attention(qkv, out, stream, batch)
         else:
-            zb.zo_attention_paged(batch.struct, self.q, nq, b.n_heads, float(b.scale), self.cache, out, out.stride(0),
-                                  self.ws, self.ws_bytes, stream)
+            zb.zo_attention_paged(batch.struct, q, ldq, b.n_heads, float(b.scale), self.cache, out, out.stride(0),
+                                  self.ws, self.ws.numel(), stream)
 
 
 class DecodeDriver:
@@ -340,7 +342,8 @@ class DecodeDriver:
            they are when they run.
     Everything a step reads lies on the device, so one captured graph replays every step; the caller fills `u` before each
     draw and reads `tokens` after it.  The caches have room for max_new tokens behind the longest prompt: what follows them is
-    not stored."""
+    not stored.  Prompts run in the model's own activations: prefill() and the model's passes go to one stream, or wait for each
+    other."""
 
     def __init__(self, model, max_new, embed=None, positions=None, temperature=1.0, top_k=None, top_p=None, min_p=None,
                  page_size=64, batch=None):
@@ -382,10 +385,16 @@ class DecodeDriver:
         self.prompts.batch = batch
         if ws > d.ws_bytes:
             self.prompts.ws_bytes, self.prompts.ws = ws, torch.empty(ws, device=dev, dtype=torch.uint8)
-        self.prompt_blocks = [CachedBlock(self.prompts, blk.blk, blk.base, c, True) for blk, c in zip(model.blocks, self.cache.structs)]
-        self.blocks = [CachedBlock(self.rows, blk.blk, blk.base, c, False) for blk, c in zip(model.blocks, self.cache.structs)]
-        self.gf, self.bf = model.gf, model.bf
         new = lambda shape, dt: torch.empty(shape, device=dev, dtype=dt)
+        for blk in model.blocks[1:]:   # (all but the first take a pending sum)
+            blk.h0 = torch.empty_like(blk.h1) if blk.h0 is None else blk.h0
+        heads = max(blk.blk.n_heads for blk in model.blocks)
+        ws = zb.zo_attention_paged_workspace_bytes(S, heads, b0.head_dim, self.cache.max_len, _dt(d.dtype))
+        scratch = new((S, heads * b0.head_dim), _tt(d.dtype)), new(max(ws, 256), torch.uint8)
+        both = list(zip(model.blocks, self.cache.structs))
+        self.prompt_blocks = [CachedBlock(self.prompts, blk, c, True) for blk, c in both]
+        self.blocks = [CachedBlock(self.rows, blk, c, False, scratch) for blk, c in both]
+        self.gf, self.bf = model.gf, model.bf
         self.prompt_final, self.prompt_last = new((batch.T, self.hidden), _tt(d.dtype)), new((S, self.hidden), _tt(d.dtype))
         self.x, self.final = (new((S, self.hidden), _tt(d.dtype)) for _ in range(2))
         self.logits = new((S, d.head.shape[0]), torch.float32)

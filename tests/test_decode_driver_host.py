@@ -106,3 +106,20 @@ def test_another_batch_has_the_models_sequences(recorder):
     dec.step()
     seeds = {args[0]._obj.dir_seed for n, args in recorder.calls if n == "zo_probe_linear" and args[0]._obj.n_dirs}
     assert seeds == {other.dir_seed.data_ptr()} and model.d.batch is b
+
+
+def test_blocks_share_what_one_of_them_uses_at_a_time(recorder):
+    """One buffer of queries and one attention workspace for all blocks' steps; prompts run in the model's activations."""
+    model = DeviceModel(DeviceWorkload(_workload(), "cpu"))
+    dec = DecodeDriver(model, 4000, page_size=16)
+    dec.prefill()
+    dec.step()
+    attend = [args for n, args in recorder.calls if n == "zo_attention_paged"]
+    assert len(attend) == 2 and len({(a[1], a[8]) for a in attend}) == 1
+    for a in attend:
+        need = zb.zo_attention_paged_workspace_bytes(dec.S, 2, 128, dec.cache.max_len, zb.ZO_BF16)
+        assert need > 256 and a[9] >= need
+    for own, prompt in zip(model.blocks, dec.prompt_blocks):
+        assert all(getattr(own, n) is getattr(prompt, n) for n in ("a1", "h1", "a2", "h2", "att", "g1", "gq", "h0"))
+        assert own.d is model.d and prompt.d is dec.prompts
+    assert len({b.h1.data_ptr() for b in dec.blocks}) == 2 and dec.blocks[0].h1.shape[0] == dec.S
