@@ -303,7 +303,11 @@ def make_cache(K, V, dtype, page_table, kv_len, host_page_table=None, host_kv_le
             raise ValueError("%s is not contiguous" % what)
     if tuple(K.shape) != tuple(V.shape) or K.dtype != V.dtype:
         raise ValueError("K and V differ in shape or type")
-    if page_table.element_size() != 4 or kv_len.element_size() != 4 or page_table.shape[0] != kv_len.shape[0]:
+    if str(K.dtype) != ("torch.bfloat16" if dtype == ZO_BF16 else "torch.float32"):   # (pools of fewer bytes would be read beyond)
+        raise ValueError("K and V are %s, not of the cache's type" % K.dtype)
+    if K.ndim != 4 or page_table.ndim != 2 or kv_len.ndim != 1:
+        raise ValueError("K and V have four dimensions, page_table two and kv_len one")
+    if any(str(t.dtype) != "torch.int32" for t in (page_table, kv_len)) or page_table.shape[0] != kv_len.shape[0]:
         raise ValueError("page_table and kv_len hold one int32 row and one int32 per sequence")
     c.n_pages, c.n_kv_heads, c.page_size, c.head_dim = (int(n) for n in K.shape)
     c.dtype, c.max_pages = dtype, int(page_table.shape[1])

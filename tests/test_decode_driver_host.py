@@ -123,3 +123,16 @@ def test_blocks_share_what_one_of_them_uses_at_a_time(recorder):
         assert all(getattr(own, n) is getattr(prompt, n) for n in ("a1", "h1", "a2", "h2", "att", "g1", "gq", "h0"))
         assert own.d is model.d and prompt.d is dec.prompts
     assert len({b.h1.data_ptr() for b in dec.blocks}) == 2 and dec.blocks[0].h1.shape[0] == dec.S
+
+
+def test_make_cache_takes_pools_of_the_stated_type_alone():
+    """A pool of two-byte values under a four-byte type would be read behind its end; lengths in floats are no lengths."""
+    K, V = torch.zeros(4, 2, 16, 8), torch.zeros(4, 2, 16, 8)
+    table, kv = torch.zeros(3, 2, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    assert zb.make_cache(K, V, zb.ZO_F32, table, kv).head_dim == 8
+    assert zb.make_cache(K.bfloat16(), V.bfloat16(), zb.ZO_BF16, table, kv).head_dim == 8
+    for k, v, dt, t, n in ((K.bfloat16(), V.bfloat16(), zb.ZO_F32, table, kv), (K, V, zb.ZO_BF16, table, kv),
+                           (K.half(), V.half(), zb.ZO_BF16, table, kv), (K, V, zb.ZO_F32, table.float(), kv),
+                           (K, V, zb.ZO_F32, table, kv.float()), (K[0], V[0], zb.ZO_F32, table, kv), (K, V, zb.ZO_F32, kv, kv)):
+        with pytest.raises(ValueError):
+            zb.make_cache(k, v, dt, t, n)
