@@ -518,7 +518,10 @@ int32_t zo_attention_paged(const zo_batch* batch, const void* Q, int64_t ldq, in
  * -infinity: token -1, prob 0, n_kept 0.  u is clamped to [0, 1] (NaN: 0).
  *   temperature, u  fp32 [n_rows];  top_k int32 [n_rows], top_p, min_p fp32 [n_rows], each may be NULL: no limit
  *   tokens int32 [n_rows];  prob fp32 [n_rows] and n_kept int32 [n_rows], each may be NULL
- * Weights and their sums are formed in 64 bits; a weight below 2^-1000 of the largest is none.  vocab up to 2^19.  The logits
+ * Weights and their sums are formed in 64 bits, each weight to 3e-13 of itself; one below 2^-1000 of the largest is none.  Where
+ * filters leave up to 4096 tokens, their sums count whole units of 2^-50 of the largest weight, at least one for every token
+ * that has a weight (prob is the token's own); top-p passes over weights below 2^-127 of the largest, which no fp32 top_p can
+ * tell from none.  vocab up to 2^19.  The logits
  * need no alignment beyond their type's.  The kernel's scratch lies in LDS: the query returns 0, and workspace may be NULL.
  */
 size_t zo_sample_workspace_bytes(int32_t n_rows, int32_t vocab, zo_dtype dtype);

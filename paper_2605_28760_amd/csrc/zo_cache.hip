@@ -154,8 +154,8 @@ __global__ __launch_bounds__(256) void k_cache_append(AppendArgs a) {
 // partners kDh/2 + 4 j .., so that the sum of squares is a few exchanges between neighbours and the rotation stays in the lane.
 // A wave takes rows (one after another where there are many) and `per_wave` groups of 512 / kDh heads of each, the next group's
 // loads under way; angles are formed once per row, frequencies once per wave.  Queries, keys and values are one list of heads.
-// Bound by memory: 17233 rows of 32 + 2 * 8 heads of 128, 96 us (4.4 TB/s;
-// a wave per row and head took 676); 16 rows: the latency of a launch.
+// Bound by memory: 17233 rows of 32 + 2 * 8 heads of 128, 93 us (4.5 TB/s; fp32 175, 4.8; a wave per row and head took 676), keys
+// and values alone 37; 16 rows: the latency of a launch.
 template <typename Tio> struct Four;
 template <> struct Four<bf16_t> {
   typedef uint2 type;
@@ -293,8 +293,8 @@ __global__ __launch_bounds__(256) void k_cache_append_heads(AppendArgs a, int pe
 //           r dh/16 + d, and a lane ends with dh/4 neighbouring columns of its query.
 // fp32 uses the 16x16x4 instruction on 16 keys per step: a lane's scores are those of keys 4 g .. 4 g + 3, and since its operands
 // are one value per lane, the values need no transposition.
-// Bound by memory where there are rows enough: 32 rows of 2048, 40 heads, 238 us (5.6 TB/s); 2 rows of 131072, 32 heads over 8, 192
-// us (5.6); 80 rows of 64..1024, 46 us (41 and the join 5).  Four waves per range 49 us, eight 58, one 49 and slower on few rows;
+// Bound by memory where there are rows enough: 32 rows of 2048, 40 heads, 238 us (5.6 TB/s); 2 rows of 131072, 32 heads over 8, 193
+// us (5.6); 80 rows of 64..1024, 46.5 us (41.5 and the join 5).  The second product of a bf16 weight costs 0.3 to 0.5 us of them.  Four waves per range 49 us, eight 58, one 49 and slower on few rows;
 // ranges of 512: 256 rows of 1000..4000 7 % faster, one row of 8000 15 % slower; one step in registers 545 -> 559 us.
 
 constexpr int kRangeWaves = 2;       // waves of a range
