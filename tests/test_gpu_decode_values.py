@@ -168,3 +168,14 @@ def test_append_in_place_without_norm_and_rotation_leaves_the_queries(dh):
     assert torch.equal(s.qkv.view(torch.int16), bits)
     _, K, V = od.cache_append(np.zeros((41, 4 * dh)), _np(s.k)[:41], _np(s.v)[:41], s.cu, 4, None, None, 0.0, 0.0, K0, V0, s.table, s.kv)
     assert (_np(s.K) == K).all() and (_np(s.V) == V).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [1, 33, 1000])
+def test_positions_alone_are_advanced(dtype, n):
+    pos = _i32(np.arange(n) * 7 - 3)
+    for alias in (False, True):
+        start, nxt = pos.clone(), torch.zeros_like(pos)
+        nxt = start if alias else nxt
+        zb.zo_embed_rows(torch.zeros_like(pos), start, n, None, 0, 0, None, 0, 0, 0, ZT[dtype], None, 0, nxt)
+        assert torch.equal(nxt, pos + 1)
